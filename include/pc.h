@@ -7,7 +7,10 @@
  * prefix-cache instances (LRU, S3-FIFO, PrefixShield) over those keys, one
  * wavefront per instance on runs of blocks, or one workgroup of four where
  * an instance does not fit that form, with admission debt metered per
- * accounting group.
+ * accounting group.  Beside them it has the pages of a real KV cache (forking,
+ * growing, freeing, compacting, storing), the groups of a batch that its
+ * block keys show to share a prefix, and attention that reads such a prefix
+ * once for its group.
  *
  * Conventions (every entry point):
  *   - Pointers named d_* are DEVICE pointers owned by the caller; they must
@@ -18,7 +21,7 @@
  *   - Return value: PC_OK (0) or a negative PC_E* code; pc_last_error()
  *     then describes the failure.  Host-side validation happens before any
  *     device work is queued; a rejected call queues nothing.
- *   - Everything is integer: keys are uint64, balances and debts are int64
+ *   - Replay and keys are integer: keys are uint64, balances and debts are int64
  *     in Q16 fixed point (2^16 = one block).
  */
 #ifndef PC_H
@@ -36,6 +39,7 @@ extern "C" {
 #define PC_EDEVICE (-3)       /* HIP runtime or launch error                          */
 #define PC_EUNSUPPORTED (-4)  /* a parameter the GPU path does not implement          */
 #define PC_EINTERNAL (-5)     /* internal table overflow (never expected)             */
+#define PC_ENOPAGES (-6)      /* a pool has too few pages that nobody holds           */
 
 #define PC_BLOCK_TOKENS 16    /* the only block size the GPU path implements          */
 #define PC_MAX_GROUPS 64
@@ -258,6 +262,175 @@ int32_t pc_replay_batch_static(const pc_trace_desc *traces, int32_t n_traces,
 int32_t pc_get_stats(const void *d_stats, int32_t n_inst, int32_t instance,
                      pc_group_stats *groups_out, int32_t max_groups,
                      pc_instance_stats *inst_out, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Pages of a KV cache, and attention over them.
+ *
+ * A pool holds the K and V of sequences in pages of PC_BLOCK_TOKENS tokens,
+ * the blocks that pc_hash_blocks keys.  Token t of a sequence is in the page
+ * table[seq][t / 16], at place t % 16.  Sequences may hold a page together
+ * (a shared prefix, a fork): refs[page] counts its holders, and a page that
+ * nobody holds has 0.  All of it is the caller's device memory; the calls
+ * below change it on the stream that they are given, and calls on one pool
+ * that change it must be ordered.
+ *
+ * Device-side status (d_status, one int32 in device memory that the caller
+ * zeroes): a call that finds its lists or the pool's state out of range sets
+ * it to PC_EINVAL, or PC_ENOPAGES, and does nothing else unless said
+ * otherwise.  A call that finds it set does nothing, so that calls may be
+ * queued one after another (or captured) and looked at once, at the end.
+ * No call reads or writes outside the buffers described here, whatever the
+ * lists and tables hold.
+ *
+ * Every call can be captured into a HIP graph.  A workspace holds nothing
+ * between calls (but for pc_attn, see there): calls that do not overlap may
+ * share one, on one stream or in several graphs.
+ * ------------------------------------------------------------------------ */
+enum { PC_BF16 = 0, PC_FP16 = 1 };
+enum { PC_HEADS_FIRST = 0,            /* a page is [n_kv_heads][16][head_dim]          */
+       PC_TOKENS_FIRST = 1 };         /* a page is [16][n_kv_heads][head_dim]          */
+
+#define PC_MAX_SEQS 262144            /* sequences of a pool                           */
+#define PC_MAX_POOL_PAGES (1 << 27)
+#define PC_MAX_BATCH 4096             /* requests of one batch                         */
+
+typedef struct {
+    void *d_k, *d_v;                  /* page 0 of layer 0, 16-byte aligned            */
+    int32_t *d_refs;                  /* [n_pages] holders                             */
+    int32_t *d_table;                 /* [n_seqs][table_width]; entries at and behind a
+                                         sequence's last page may hold anything        */
+    int32_t *d_len;                   /* [n_seqs] tokens, 0..16 * table_width          */
+    int64_t page_stride;              /* elements from a page to the next, >= one
+                                         page's 16 * n_kv_heads * head_dim, a multiple
+                                         of 8; the same for K and V                    */
+    int64_t layer_stride;             /* elements from a layer to the next, a multiple
+                                         of 8 (any value where n_layers is 1)          */
+    int32_t n_layers;                 /* >= 1; the layers share table, len and refs    */
+    int32_t n_pages;                  /* 1..PC_MAX_POOL_PAGES                          */
+    int32_t n_seqs;                   /* 1..PC_MAX_SEQS                                */
+    int32_t table_width;              /* 1..2^24                                       */
+    int32_t n_kv_heads;               /* 1..256                                        */
+    int32_t head_dim;                 /* 64 or 128                                     */
+    int32_t dtype;                    /* PC_BF16 / PC_FP16                             */
+    int32_t layout;                   /* PC_HEADS_FIRST / PC_TOKENS_FIRST              */
+} pc_pages;
+
+/* Rows of K, V, queries or results: one of head_dim elements (contiguous, 16-byte
+ * aligned) for each token and head. */
+typedef struct {
+    void *d_data;
+    int64_t token_stride, head_stride;   /* elements, multiples of 8 */
+} pc_rows;
+
+/* Workspace bytes of pc_pages_extend for up to n sequences a call, and of
+ * pc_pages_compact (any n >= 0).  < 0: invalid, see pc_last_error. */
+int64_t pc_pages_workspace_bytes(const pc_pages *pages, int64_t n);
+
+/* Child i takes over parent i's pages and length; each page has a holder
+ * more.  A parent may have several children.  Children are distinct, empty
+ * (length 0), and no parents. */
+int32_t pc_pages_fork(const pc_pages *pages, const int32_t *d_parent, const int32_t *d_child, int32_t n,
+                      int32_t *d_status, void *stream);
+
+/* Sequence d_seq[i] grows by d_add[i] >= 0 tokens; the sequences are distinct.
+ * New pages are the lowest that nobody holds, handed out in the order of the
+ * list.  A last page that is filled in part and held by others too is copied
+ * for a sequence that grows, K and V of every layer, the copy taking the first
+ * of its new pages; but where all its holders are in the list and grow, the
+ * first of them keeps it.  The pages that hold the new tokens are then the
+ * sequence's alone.  Their K and V are as they were: pc_pages_write fills them.
+ * A pool with too few pages sets the status to PC_ENOPAGES and is left as it was.
+ *   d_workspace   pc_pages_workspace_bytes(pages, n) bytes, 256-byte aligned */
+int32_t pc_pages_extend(const pc_pages *pages, const int32_t *d_seq, const int32_t *d_add, int32_t n,
+                        void *d_workspace, int64_t workspace_bytes, int32_t *d_status, void *stream);
+
+/* The distinct sequences d_seq[i] give their pages up (a holder less each) and
+ * are empty.  Their table entries and the pages' K and V stay as they are
+ * until the pages are handed out again. */
+int32_t pc_pages_free(const pc_pages *pages, const int32_t *d_seq, int32_t n, int32_t *d_status, void *stream);
+
+/* Pages in use move to the lowest page numbers: with n_live pages in use, the
+ * i-th one at or behind n_live moves to the i-th unused place before it, K and
+ * V of every layer.  New counts and tables go to d_refs_to [n_pages] and
+ * d_table_to [n_seqs][table_width] (which may be the pool's own), n_live to
+ * d_n_live.  Where they are not the pool's own, readers of the old table find
+ * what they did: pages that moved keep their contents at the old place.
+ * A page number out of the pool, or of a page that nobody holds, is passed on
+ * as it is and sets the status to PC_EINVAL. */
+int32_t pc_pages_compact(const pc_pages *pages, int32_t *d_refs_to, int32_t *d_table_to, int32_t *d_n_live,
+                         void *d_workspace, int64_t workspace_bytes, int32_t *d_status, void *stream);
+
+/* Stores K and V of the last tokens of n distinct sequences, in one layer: rows
+ * d_new_off[i] .. d_new_off[i+1]-1 of k_new and v_new (n_tokens rows) are the
+ * last tokens of sequence d_seq[i], which pc_pages_extend has made room for.
+ * Where the status is set, rows may or may not have been stored: a token's page
+ * out of the pool, or held by more than one sequence, is not written. */
+int32_t pc_pages_write(const pc_pages *pages, int32_t layer, const int32_t *d_seq, const int32_t *d_new_off,
+                       int32_t n, int64_t n_tokens, const pc_rows *k_new, const pc_rows *v_new,
+                       int32_t *d_status, void *stream);
+
+/* Groups of a batch by the block keys of its requests (d_keys, d_key_off: as
+ * of pc_block_offsets and pc_hash_blocks).  Two requests with at least
+ * min_blocks >= 1 full blocks are in one group if their keys of block
+ * min_blocks - 1 are equal (keys are chained, so their blocks before it are
+ * then equal too); a request with fewer blocks is in a group of its own.
+ * Groups are in the order of their first requests, requests in a group in
+ * their own order:
+ *   d_order      [n_req] the requests, group by group
+ *   d_group_off  [n_req+1] group g: d_order[d_group_off[g]] .. ; n_req from
+ *                d_group_off[n_groups] on
+ *   d_shared     [n_req] leading blocks with the same keys in all requests of
+ *                group g; 0 for a group of one and behind the last group
+ *   d_n_groups   [1]
+ * n_req is at most PC_MAX_BATCH (else PC_EUNSUPPORTED).  d_status: PC_EINVAL
+ * if the offsets fall, or leave [0, n_keys]. */
+int32_t pc_prefix_groups(const uint64_t *d_keys, int64_t n_keys, const int64_t *d_key_off, int32_t n_req,
+                         int32_t min_blocks, int32_t *d_order, int32_t *d_group_off, int32_t *d_shared,
+                         int32_t *d_n_groups, int32_t *d_status, void *stream);
+
+/* Attention of a batch over its pages, in two calls: a plan, once for a batch
+ * of the lengths it then has, and the attention of one layer by that plan, as
+ * often as there are layers.
+ *   request r     the sequence d_seq[r] (one may come twice) and the queries
+ *                 d_q_off[r] .. d_q_off[r+1]-1 of n_tokens; its length L counts
+ *                 the tokens of these queries, whose K and V are in the pages.
+ *   causal        query i of n sees the tokens before L - n + i + 1; otherwise,
+ *                 all L.  A query that sees none (also: of an empty sequence)
+ *                 gives zeros, and -inf in lse.
+ *   d_order ..    the groups, as pc_prefix_groups gives them; or all four NULL:
+ *                 no request shares anything.  The pages of a group's shared
+ *                 blocks have to hold the same tokens in all its requests: those
+ *                 of the first one are read for all.  Shared blocks behind the
+ *                 shortest request's last full one are taken as not shared.
+ * A group's shared tokens are read once for the queries of all its requests,
+ * each request's own tokens by itself, and long ranges in several parts; the
+ * results are joined by their sums of exponentials.  Scores, sums and joined
+ * values are in 32 bits; the weights are rounded to the pool's type before
+ * the product with V.  Results do not depend on timing.
+ * K of a token that a query does not see, and K and V behind the length, may
+ * hold anything.  V of the tokens within the length is finite: a weight of
+ * zero times infinity or NaN is NaN.
+ *   d_workspace   pc_attn_workspace_bytes() bytes, 256-byte aligned; it holds the
+ *                 plan from pc_attn_plan until the last pc_attn of that plan
+ *                 is done. */
+int64_t pc_attn_workspace_bytes(const pc_pages *pages, int32_t n_req, int64_t n_tokens, int32_t n_heads);
+
+int32_t pc_attn_plan(const pc_pages *pages, const int32_t *d_seq, const int32_t *d_q_off, int32_t n_req,
+                     int64_t n_tokens, int32_t n_heads, int32_t causal, const int32_t *d_order,
+                     const int32_t *d_group_off, const int32_t *d_shared, const int32_t *d_n_groups,
+                     void *d_workspace, int64_t workspace_bytes, int32_t *d_status, void *stream);
+
+/* out[t][h] = softmax(scale * q[t][h] . K) V over the tokens that query t sees;
+ * n_heads is a multiple of the KV heads, head h reads KV head
+ * h / (n_heads / n_kv_heads).  n_req, n_tokens and n_heads are the plan's, and so
+ * are the pool's table and lengths; K and V are of `layer`.  scale > 0.
+ *   d_lse         optional (NULL): [n_tokens][n_heads] float, the natural
+ *                 logarithm of each row's sum of exponentials
+ * By a plan that set the status, nothing is written.  A page number out of
+ * the pool reads another page, never memory outside. */
+int32_t pc_attn(const pc_pages *pages, int32_t layer, const pc_rows *q, int32_t n_req, int64_t n_tokens,
+                int32_t n_heads, float scale, const pc_rows *out, float *d_lse, void *d_workspace,
+                int64_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

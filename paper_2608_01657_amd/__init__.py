@@ -1,8 +1,9 @@
 """MI355X-native batched replay of a multi-tenant KV prefix cache (PrefixShield).
 
 Thin ctypes binding over libpcreplay.so (C ABI in include/pc.h).  Every
-function here only marshals arguments; block cutting, hashing and replay run
-in the library's HIP kernels.  PyTorch provides device memory and streams.
+function here only marshals arguments; block cutting, hashing, replay, the
+page operators and the attention over shared prefixes run in the library's
+HIP kernels.  PyTorch provides device memory and streams.
 
 The library is loaded from this package directory; if it is missing the
 first call raises -- there is no CPU fallback.
@@ -26,6 +27,7 @@ PHASE_NAMES = ["request_start", "lookup", "reclamation", "charge", "insert_relea
 PHASE_EVENTS = ["evicting_requests", "log_compactions", "s3fifo_scan_batches", "prefixshield_queue_takes"]
 
 PC_OK, PC_EINVAL, PC_ENOMEM, PC_EDEVICE, PC_EUNSUPPORTED, PC_EINTERNAL = 0, -1, -2, -3, -4, -5
+PC_ENOPAGES = -6
 PC_BLOCK_TOKENS = 16
 PC_MAX_GROUPS, PC_MAX_CONTRACTS, PC_MAX_CAPACITY = 64, 4, 32767
 PC_LRU, PC_S3FIFO, PC_PREFIXSHIELD, PC_STATICQUOTA = 0, 1, 2, 3
@@ -33,6 +35,9 @@ PC_FLAG_NO_SEGMENTATION, PC_FLAG_NO_DEBT_GATE = 1, 2
 PC_STATS_RECORD_BYTES = 64 * 136 + 64
 PC_ROUTE_GENERAL, PC_ROUTE_RUNS, PC_ROUTE_RUNS_WIDE = 0, 1, 2
 PC_LAYOUT_LDS, PC_LAYOUT_HYBRID, PC_LAYOUT_WS = 0, 1, 2
+PC_BF16, PC_FP16 = 0, 1
+PC_HEADS_FIRST, PC_TOKENS_FIRST = 0, 1
+PC_MAX_SEQS, PC_MAX_POOL_PAGES, PC_MAX_BATCH = 262144, 1 << 27, 4096
 LAYOUT_NAMES = {PC_LAYOUT_LDS: "lds", PC_LAYOUT_HYBRID: "hybrid", PC_LAYOUT_WS: "workspace"}
 
 GROUP_FIELDS = ["requests", "probes", "hits", "misses", "charged", "evicted_owned",
@@ -68,6 +73,18 @@ class pc_instance_desc(ctypes.Structure):
                 ("contract", pc_contract * 4)]
 
 
+class pc_pages(ctypes.Structure):
+    _fields_ = [("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_refs", ctypes.c_void_p),
+                ("d_table", ctypes.c_void_p), ("d_len", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("layer_stride", ctypes.c_int64), ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("n_seqs", ctypes.c_int32), ("table_width", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("layout", ctypes.c_int32)]
+
+
+class pc_rows(ctypes.Structure):
+    _fields_ = [("d_data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
 class pc_group_stats(ctypes.Structure):
     _fields_ = [(f, ctypes.c_uint64) for f in GROUP_FIELDS[:12]] + \
                [(f, ctypes.c_int64) for f in GROUP_FIELDS[12:]]
@@ -81,7 +98,9 @@ class pc_instance_stats(ctypes.Structure):
 
 EXPORTS = ["pc_last_error", "pc_block_offsets", "pc_hash_blocks", "pc_replay_workspace_bytes",
            "pc_replay_workspace_min_bytes", "pc_replay_route_offset", "pc_replay_state_bytes", "pc_replay_batch",
-           "pc_replay_batch_static", "pc_get_stats"]
+           "pc_replay_batch_static", "pc_get_stats", "pc_pages_workspace_bytes", "pc_pages_fork", "pc_pages_extend",
+           "pc_pages_free", "pc_pages_compact", "pc_pages_write", "pc_prefix_groups", "pc_attn_workspace_bytes",
+           "pc_attn_plan", "pc_attn"]
 PC_STATIC_WORKSPACE_BYTES = 64 << 20
 
 _lib = None
@@ -151,6 +170,20 @@ def lib():
         L.pc_get_stats.restype = i32
         L.pc_get_stats.argtypes = [P, i32, i32, ctypes.POINTER(pc_group_stats), i32,
                                    ctypes.POINTER(pc_instance_stats), P]
+        G, W = ctypes.POINTER(pc_pages), ctypes.POINTER(pc_rows)
+        for name, res, args in (
+                ("pc_pages_workspace_bytes", i64, [G, i64]),
+                ("pc_pages_fork", i32, [G, P, P, i32, P, P]),
+                ("pc_pages_extend", i32, [G, P, P, i32, P, i64, P, P]),
+                ("pc_pages_free", i32, [G, P, i32, P, P]),
+                ("pc_pages_compact", i32, [G, P, P, P, P, i64, P, P]),
+                ("pc_pages_write", i32, [G, i32, P, P, i32, i64, W, W, P, P]),
+                ("pc_prefix_groups", i32, [P, i64, P, i32, i32, P, P, P, P, P, P]),
+                ("pc_attn_workspace_bytes", i64, [G, i32, i64, i32]),
+                ("pc_attn_plan", i32, [G, P, P, i32, i64, i32, i32, P, P, P, P, P, i64, P, P]),
+                ("pc_attn", i32, [G, i32, W, i32, i64, i32, ctypes.c_float, W, P, P, i64, P])):
+            f = getattr(L, name)
+            f.restype, f.argtypes = res, args
         _lib = L
     return _lib
 
@@ -260,6 +293,76 @@ def pc_get_stats(stats, n_inst: int, instance: int = -1, max_groups: int = 64, s
     return G, S
 
 
+def _bytes(t) -> int:
+    return int(t.numel() * t.element_size())
+
+
+def _size(v: int) -> int:
+    if v < 0:
+        _check(int(v))
+    return int(v)
+
+
+def pc_pages_workspace_bytes(pages: pc_pages, n: int) -> int:
+    return _size(lib().pc_pages_workspace_bytes(pages, n))
+
+
+def pc_pages_fork(pages: pc_pages, parent, child, status, stream=None):
+    """Child i takes over parent i's pages and length (int32 device tensors)."""
+    return _check(lib().pc_pages_fork(pages, _ptr(parent), _ptr(child), int(child.numel()), _ptr(status),
+                                      _stream(stream)))
+
+
+def pc_pages_extend(pages: pc_pages, seq, add, workspace, status, stream=None):
+    """Sequence seq[i] grows by add[i] tokens."""
+    return _check(lib().pc_pages_extend(pages, _ptr(seq), _ptr(add), int(seq.numel()), _ptr(workspace),
+                                        _bytes(workspace), _ptr(status), _stream(stream)))
+
+
+def pc_pages_free(pages: pc_pages, seq, status, stream=None):
+    """The sequences give their pages up and are empty."""
+    return _check(lib().pc_pages_free(pages, _ptr(seq), int(seq.numel()), _ptr(status), _stream(stream)))
+
+
+def pc_pages_compact(pages: pc_pages, refs_to, table_to, n_live, workspace, status, stream=None):
+    """Pages in use move to the lowest page numbers."""
+    return _check(lib().pc_pages_compact(pages, _ptr(refs_to), _ptr(table_to), _ptr(n_live), _ptr(workspace),
+                                         _bytes(workspace), _ptr(status), _stream(stream)))
+
+
+def pc_pages_write(pages: pc_pages, layer: int, seq, new_off, n_tokens: int, k_new: pc_rows, v_new: pc_rows, status,
+                   stream=None):
+    """K and V of the sequences' last tokens stored in their pages."""
+    return _check(lib().pc_pages_write(pages, layer, _ptr(seq), _ptr(new_off), int(seq.numel()), n_tokens, k_new,
+                                       v_new, _ptr(status), _stream(stream)))
+
+
+def pc_prefix_groups(keys, key_off, min_blocks: int, order, group_off, shared, n_groups, status, stream=None):
+    """Groups of a batch whose block keys begin alike, and how many blocks each shares."""
+    return _check(lib().pc_prefix_groups(_ptr(keys), int(keys.numel()), _ptr(key_off), int(key_off.numel()) - 1,
+                                         min_blocks, _ptr(order), _ptr(group_off), _ptr(shared), _ptr(n_groups),
+                                         _ptr(status), _stream(stream)))
+
+
+def pc_attn_workspace_bytes(pages: pc_pages, n_req: int, n_tokens: int, n_heads: int) -> int:
+    return _size(lib().pc_attn_workspace_bytes(pages, n_req, n_tokens, n_heads))
+
+
+def pc_attn_plan(pages: pc_pages, seq, q_off, n_tokens: int, n_heads: int, causal: bool, order, group_off, shared,
+                 n_groups, workspace, status, stream=None):
+    """The plan of a batch's attention, for all layers (groups: all four, or None)."""
+    return _check(lib().pc_attn_plan(pages, _ptr(seq), _ptr(q_off), int(seq.numel()), n_tokens, n_heads, int(causal),
+                                     _ptr(order), _ptr(group_off), _ptr(shared), _ptr(n_groups), _ptr(workspace),
+                                     _bytes(workspace), _ptr(status), _stream(stream)))
+
+
+def pc_attn(pages: pc_pages, layer: int, q: pc_rows, n_req: int, n_tokens: int, n_heads: int, scale: float,
+            out: pc_rows, lse, workspace, stream=None):
+    """Attention of one layer by the plan in the workspace."""
+    return _check(lib().pc_attn(pages, layer, q, n_req, n_tokens, n_heads, scale, out, _ptr(lse), _ptr(workspace),
+                                _bytes(workspace), _stream(stream)))
+
+
 # --------------------------------------------------------------------------
 # Descriptor builders (host structs pointing at device tensors)
 # --------------------------------------------------------------------------
@@ -269,6 +372,22 @@ def make_trace_desc(keys, key_off, group, contract, prefix, n_groups, n_prefix, 
     return pc_trace_desc(_ptr(keys), _ptr(key_off), _ptr(group), _ptr(contract), _ptr(prefix), _ptr(tick),
                          int(group.numel()), int(keys.numel()), int(n_prefix), int(n_groups),
                          int(max_req_blocks))
+
+
+def make_pages(k, v, refs, table, length, tokens_first: bool = False) -> pc_pages:
+    """k, v: [layers, pages, heads, 16, dim], or [layers, pages, 16, heads, dim] with tokens_first."""
+    import torch
+    L, n, a, b, D = k.shape
+    heads = b if tokens_first else a
+    return pc_pages(_ptr(k), _ptr(v), _ptr(refs), _ptr(table), _ptr(length), k.stride(1), k.stride(0), L, n,
+                    int(table.shape[0]), int(table.shape[1]), heads, D,
+                    {torch.bfloat16: PC_BF16, torch.float16: PC_FP16}.get(k.dtype, -1),
+                    PC_TOKENS_FIRST if tokens_first else PC_HEADS_FIRST)
+
+
+def make_rows(x) -> pc_rows:
+    """x: [tokens, heads, dim], dim contiguous."""
+    return pc_rows(_ptr(x), x.stride(0), x.stride(1))
 
 
 def make_instance_desc(inst) -> pc_instance_desc:

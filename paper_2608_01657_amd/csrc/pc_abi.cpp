@@ -14,14 +14,15 @@
 #include <vector>
 
 #include "pc.h"
+#include "pc_host.h"
 #include "pc_internal.h"
 
 #define PC_RUNS_FN inline
 #include "pc_runs.h"
 
-namespace {
+static thread_local std::string g_err;
 
-thread_local std::string g_err;
+namespace pcr {
 
 int32_t fail(int32_t code, const char *fmt, ...) {
     char buf[512];
@@ -39,6 +40,14 @@ int32_t ok() {
 int32_t hip_fail(hipError_t e, const char *what) {
     return fail(PC_EDEVICE, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace pcr
+
+using pcr::fail;
+using pcr::hip_fail;
+using pcr::ok;
+
+namespace {
 
 int ceil_log2(int64_t v) {
     int b = 0;

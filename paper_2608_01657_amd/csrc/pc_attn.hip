@@ -1,0 +1,707 @@
+// pc_attn.hip -- attention over paged K and V on gfx950, a batch's shared
+// prefixes read once for all their requests.
+//
+// A batch is cut into segments: a group's queries against its shared tokens,
+// and each request's queries against its own.  A segment is a small dense
+// problem: rows (a query and one of the query heads of a KV head) against
+// tokens.  Rows are cut into tiles, long token ranges into chunks (the plan),
+// and every (tile, KV head, chunk) is one item.  Per item
+//   m = max s,  l = sum 2^(s - m),  o = sum 2^(s - m) v / l,  s = q.k scale log2(e)
+// in one pass over the tokens with a running m and l.  Items of one row are
+// joined by w_i = 2^(lse_i - max lse), lse_i = m_i + log2(l_i).
+//
+// Both kernels form S^T = K Q^T and O^T = V^T P^T, so that a lane holds scores
+// of one query in registers: the running statistics need one exchange between
+// lane halves (or quarters), the scaling of O^T none, and P^T is the B operand
+// of the second product as it lies, once the order of the tokens inside a
+// matrix instruction's k is taken to be the order in which the first product
+// leaves them.  V^T comes from row-major V by the transposing LDS read.
+#include "pc_pages.h"
+
+namespace pcr {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+struct Bf16 {
+    typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+    static __device__ f32x16 mma32(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    }
+    static __device__ f32x4 mma16(s16x8 a, s16x8 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    }
+    // to nearest, ties to even
+    static __device__ uint32_t pack(float a, float b) {
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+    }
+};
+struct Fp16 {
+    typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+    static __device__ f32x16 mma32(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    }
+    static __device__ f32x4 mma16(s16x8 a, s16x8 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    }
+    static __device__ uint32_t pack(float a, float b) {
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
+    }
+};
+
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNegInf = -__builtin_inff();
+
+using as1 = __attribute__((address_space(1))) void;
+using as3 = __attribute__((address_space(3))) void;
+
+__device__ __forceinline__ void load_lds16(const void *g, void *l) {
+    __builtin_amdgcn_global_load_lds((const as1 *)g, (as3 *)l, 16, 0, 0);
+}
+__device__ __forceinline__ s16x4 read_tr(const uint16_t *l) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)l);
+}
+__device__ __forceinline__ s16x8 join(s16x4 a, s16x4 b) {
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
+
+// Every load of the wave has landed in LDS.
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// The item of a workgroup's (or wave's) turn: workgroups go round the eight
+// XCDs, and neighbouring items (row tiles of the same tokens) share an L2
+// where they are on one.
+__device__ __forceinline__ int xcd_item(int turn, int n) {
+    const int per = (n + 7) / 8, at = (turn & 7) * per + (turn >> 3);
+    return turn >> 3 < per && at < n ? at : -1;
+}
+__device__ __forceinline__ int xcd_turns(int n) { return (n + 7) / 8 * 8; }
+
+// ------------------------------------------------------------------ plan
+
+constexpr int kPlanThreads = 1024;
+
+template <typename N>
+__device__ N plan_sum(N v, N *total, N *lds) {    // exclusive, over the workgroup
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    N x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const N y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 63) lds[w] = x;
+    __syncthreads();
+    N before = 0, all = 0;
+    for (int i = 0; i < kPlanThreads / 64; ++i) {
+        const N t = lds[i];
+        if (i < w) before += t;
+        all += t;
+    }
+    *total = all;
+    return before + x - v;
+}
+
+// One workgroup makes the list of items.  Segment i < n_req is the own tokens
+// of the request at place i of the order, segment n_req + g group g's shared
+// tokens.
+__global__ __launch_bounds__(kPlanThreads) void attn_plan(AttnPlanArgs a) {
+    const pc_pages &p = a.p;
+    const AttnWs &ws = a.ws;
+    const int R = a.n_req, S = 2 * R + 2, G = a.n_heads / p.n_kv_heads, Hk = p.n_kv_heads;
+    int32_t *t0 = ws.place, *n_tok = t0 + S, *kv0 = n_tok + S, *kv1 = kv0 + S, *seq = kv1 + S, *gof = seq + S,
+            *len_at = gof + S;
+    __shared__ int lds[kPlanThreads / 64];
+    __shared__ int64_t lds64[kPlanThreads / 64];
+    __shared__ int any_bad;
+    __shared__ uint32_t seen[PC_MAX_BATCH / 32];
+    const int tid = threadIdx.x;
+    if (tid < PC_MAX_BATCH / 32) seen[tid] = 0;
+    if (tid == 0) {
+        any_bad = *a.status != PC_OK;
+        *ws.head = AttnHead{0, 0, 0, 0};
+    }
+    if (tid < 32) reinterpret_cast<int32_t *>(reinterpret_cast<char *>(ws.head) + kZeroOffset)[tid] = 0;
+    __syncthreads();
+    if (any_bad) return;
+    // the requests at their places
+    const bool grouped = a.order != nullptr;
+    const int n_groups = grouped ? *a.n_groups : 0;
+    bool bad = n_groups < 0 || n_groups > R;
+    int64_t total = 0;
+    for (int j0 = 0; j0 < R; j0 += kPlanThreads) {
+        const int j = j0 + tid;
+        int n = 0, q0 = 0, s = 0, len = 0;
+        if (j < R) {
+            const uint32_t r = grouped ? (uint32_t)a.order[j] : (uint32_t)j;
+            if (r >= (uint32_t)R || (atomicOr(&seen[r >> 5], 1u << (r & 31)) >> (r & 31) & 1)) {
+                bad = true;
+            } else {
+                q0 = a.q_off[r];
+                n = a.q_off[r + 1] - q0;
+                s = a.seq[r];
+                if (q0 < 0 || n < 0 || (int64_t)q0 + n > a.n_tokens || (uint32_t)s >= (uint32_t)p.n_seqs) bad = true;
+                else len = p.d_len[s];
+                if (len < 0 || (int64_t)len > (int64_t)p.table_width * kBlk) bad = true;
+            }
+            if (bad) n = 0;
+        }
+        int64_t all;
+        const int at = (int)(total + plan_sum((int64_t)n, &all, lds64));
+        if (j < R) {
+            t0[j] = at;
+            n_tok[j] = n;
+            seq[j] = s;
+            kv0[j] = 0;
+            kv1[j] = len;
+            gof[j] = q0;        // until the queries are listed
+            len_at[j] = len;
+        }
+        total += all;
+    }
+    if (total != a.n_tokens) bad = true;    // every request once, so every query in one request
+    if (bad) any_bad = 1;
+    __syncthreads();
+    if (any_bad) {
+        if (tid == 0) *a.status = PC_EINVAL;
+        return;
+    }
+    // queries in the order
+    const int lane = tid & 63, wave = tid >> 6;
+    for (int j = wave; j < R; j += kPlanThreads / 64) {
+        const int n = n_tok[j], q0 = gof[j], len = len_at[j], at = t0[j];
+        for (int i = lane; i < n; i += 64) {
+            ws.tok[at + i] = q0 + i;
+            ws.lim[at + i] = a.causal ? len - n + i + 1 : len;
+            ws.pos[at + i] = j;
+        }
+    }
+    __syncthreads();
+    for (int j = tid; j < R; j += kPlanThreads) gof[j] = -1;
+    __syncthreads();
+    // groups, a wave each: the tokens that all members share
+    for (int g = wave; g < n_groups; g += kPlanThreads / 64) {
+        const int j0 = a.group_off[g], j1 = a.group_off[g + 1];
+        if (j0 < 0 || j1 < j0 || j1 > R || (g == 0 && j0 != 0) || (g == n_groups - 1 && j1 != R)) {
+            any_bad = 1;
+            continue;
+        }
+        int least = 0x7fffffff, rows = 0;
+        for (int j = j0 + lane; j < j1; j += 64) {
+            const int len = len_at[j];
+            least = len < least ? len : least;
+            rows += n_tok[j];
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) {
+            const int y = __shfl_xor(least, d);
+            least = y < least ? y : least;
+            rows += __shfl_xor(rows, d);
+        }
+        const int blocks = a.shared[g];
+        int tokens = j1 - j0 < 2 || blocks <= 0 ? 0 : least / kBlk * kBlk;
+        if ((int64_t)blocks * kBlk < tokens) tokens = blocks * kBlk;
+        const int s = R + g;
+        if (lane == 0) {
+            t0[s] = j1 > j0 ? t0[j0] : 0;
+            n_tok[s] = tokens ? rows : 0;
+            kv0[s] = 0;
+            kv1[s] = tokens;
+            seq[s] = j1 > j0 ? seq[j0] : 0;
+        }
+        if (tokens)
+            for (int j = j0 + lane; j < j1; j += 64) {
+                kv0[j] = tokens;
+                gof[j] = g;
+            }
+    }
+    __syncthreads();
+    if (any_bad) {
+        if (tid == 0) *a.status = PC_EINVAL;
+        return;
+    }
+    // blocks of work on each list, and from them how long an item may be
+    const int n_seg = R + n_groups;
+    int64_t wide = 0, narrow = 0;
+    for (int s = tid; s < n_seg; s += kPlanThreads) {
+        const int64_t rows = (int64_t)n_tok[s] * G, blocks = (kv1[s] - kv0[s] + kTileKv - 1) / kTileKv;
+        if (rows > kNarrowRows) wide += (rows + kWideRows - 1) / kWideRows * blocks;
+        else if (rows) narrow += blocks;
+    }
+    int64_t all_wide, all_narrow;
+    plan_sum(wide, &all_wide, lds64);
+    plan_sum(narrow, &all_narrow, lds64);
+    const int64_t by_wide = (all_wide * Hk + kWideItems - 1) / kWideItems,
+                  by_narrow = (all_narrow * Hk + kNarrowItems - 1) / kNarrowItems;
+    const int len_wide = (int)(by_wide < kWideMinBlocks ? kWideMinBlocks : by_wide);
+    const int len_narrow = (int)(by_narrow < kNarrowMinBlocks ? kNarrowMinBlocks : by_narrow);
+    int n_wide = 0, n_narrow = 0, rows_at = 0;
+    // groups before the requests' own tokens: theirs are the longest items
+    for (int i0 = 0; i0 < n_seg; i0 += kPlanThreads) {
+        const int i = i0 + tid, s = i < n_groups ? R + i : i - n_groups;
+        int chunks = 0, tiles = 0, per = 0, part = 0, st = 0, sn = 0, sb = 0, se = 0, ss = 0;
+        bool is_wide = false, direct = false;
+        if (i < n_seg) {
+            st = t0[s];
+            sn = n_tok[s];
+            sb = kv0[s];
+            se = kv1[s];
+            ss = seq[s];
+            const int64_t rows = (int64_t)sn * G;
+            const int blocks = (se - sb + kTileKv - 1) / kTileKv;
+            is_wide = rows > kNarrowRows;
+            if (rows && blocks) {
+                tiles = (int)((rows + kWideRows - 1) / kWideRows);
+                const int most = is_wide ? len_wide : len_narrow;
+                chunks = (blocks + most - 1) / most;
+                per = (blocks + chunks - 1) / chunks;
+                chunks = (blocks + per - 1) / per;
+                direct = s < R && chunks == 1 && gof[s] < 0;
+                part = direct ? 0 : chunks * sn * a.n_heads;
+            }
+        }
+        const int items = chunks * tiles * Hk;
+        int all_w, all_n, all_r;
+        const int at_w = n_wide + plan_sum(is_wide ? items : 0, &all_w, lds);
+        const int at_n = n_narrow + plan_sum(is_wide ? 0 : items, &all_n, lds);
+        const int at_r = rows_at + plan_sum(part, &all_r, lds);
+        n_wide += all_w;
+        n_narrow += all_n;
+        rows_at += all_r;
+        const int at = is_wide ? at_w : at_n;
+        if (i < n_seg)      // own: at the request's place; groups': behind both lists, for now
+            ws.parts[s < R ? s : R + s] = direct ? AttnParts{-1, -1, 0, 0} : AttnParts{at_r, chunks, sn, st};
+        // the items of a wave's segments, one segment after the other
+        for (uint64_t left = __ballot(items > 0); left; left &= left - 1) {
+            const int k = __ffsll((unsigned long long)left) - 1;
+            const int xn = __shfl(items, k), xt = __shfl(tiles, k), xp = __shfl(per, k) * kTileKv, xa = __shfl(at, k);
+            const int x0 = __shfl(st, k), x1 = __shfl(sn, k), xb = __shfl(sb, k), xe = __shfl(se, k);
+            const int xs = __shfl(ss, k), xr = __shfl(at_r, k), xd = __shfl((int)direct, k);
+            AttnItem *to = (__shfl((int)is_wide, k) ? ws.wide : ws.narrow) + xa;
+            for (int x = lane; x < xn; x += 64) {
+                const int tile = x % xt, rest = x / xt, head = rest % Hk, c = rest / Hk;
+                const int b = xb + c * xp;
+                to[x] = AttnItem{x0, x1, b, b + xp < xe ? b + xp : xe, xs, head | tile << 8,
+                                 xd ? -1 : xr + c * x1 * a.n_heads, 0};
+            }
+        }
+    }
+    __syncthreads();
+    for (int j = tid; j < R; j += kPlanThreads)
+        ws.parts[R + j] = gof[j] < 0 ? AttnParts{0, 0, 0, 0} : ws.parts[2 * R + gof[j]];
+    if (tid == 0) *ws.head = AttnHead{1, n_wide, n_narrow, 0};
+}
+
+// ------------------------------------------------------------------ wide items
+
+// A workgroup of four waves takes 128 rows, a wave 32 of them (the columns of
+// 32 x 32 x 16 products), and 64 tokens of K and V at a time from LDS, where a
+// second pair of buffers fills meanwhile.  16-byte pieces of a token's row are
+// permuted in LDS so that neither the row reads of K nor the transposing reads
+// of V meet in a bank: piece c of token t of K is at c ^ t, of V at c ^ 2t
+// (modulo the pieces of a row).
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void attn_wide(AttnArgs a) {
+    constexpr int kPieces = D / 8, kSteps = D / 16, kDb = D / 32;
+    __shared__ __align__(1024) uint16_t lds_k[2][kTileKv * D];
+    __shared__ __align__(1024) uint16_t lds_v[2][kTileKv * D];
+    __shared__ int lds_lim[4];
+    if (!a.ws.head->ok) return;
+    const int n_items = a.ws.head->n_wide;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const uint16_t *zeros = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(a.ws.head) + kZeroOffset);
+    const uint16_t *kp = static_cast<const uint16_t *>(a.k), *vp = static_cast<const uint16_t *>(a.v);
+    for (int turn = blockIdx.x; turn < xcd_turns(n_items); turn += gridDim.x) {
+        const int which = xcd_item(turn, n_items);
+        if (which < 0) continue;
+        const AttnItem it = a.ws.wide[which];
+        const int head = it.head_tile & 255, tile = it.head_tile >> 8;
+        const int row = tile * kWideRows + wave * 32 + col;
+        const int tok = row / a.group, hq = head * a.group + row - tok * a.group;
+        const bool active = tok < it.n_tok;
+        const int lim = active ? min(a.ws.lim[it.t0 + tok], it.kv1) : 0;
+        const int64_t q_row = active ? a.ws.tok[it.t0 + tok] : 0;
+        s16x8 qf[kSteps];
+        {
+            const uint16_t *q = static_cast<const uint16_t *>(a.q) + q_row * a.q_token + hq * a.q_head + half * 8;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+                qf[s] = active ? *reinterpret_cast<const s16x8 *>(q + 16 * s) : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        }
+        int most = lim, least = lim;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            most = max(most, __shfl_xor(most, d));
+            least = min(least, __shfl_xor(least, d));
+        }
+        least = __builtin_amdgcn_readfirstlane(least);
+        __syncthreads();        // the last item's readers of LDS
+        if (lane == 0) lds_lim[wave] = most;
+        __syncthreads();
+        const int end = __builtin_amdgcn_readfirstlane(max(max(lds_lim[0], lds_lim[1]), max(lds_lim[2], lds_lim[3])));
+        const int tiles = end > it.kv0 ? (end - it.kv0 + kTileKv - 1) / kTileKv : 0;
+        const int32_t *table = a.table + (int64_t)it.seq * a.table_width;
+
+        // a wave loads one page of each tile: 16 tokens
+        auto fetch = [&](int n, int buf) {
+            const int t_first = it.kv0 + n * kTileKv + wave * kBlk;
+            const int page_at = min(t_first, end - 1) / kBlk;
+            const uint32_t page = min((uint32_t)table[page_at], (uint32_t)(a.n_pages - 1));
+            const int64_t from = (int64_t)page * a.page_stride + (int64_t)head * a.head_stride;
+            uint16_t *lk = &lds_k[buf][wave * kBlk * D], *lv = &lds_v[buf][wave * kBlk * D];
+#pragma unroll
+            for (int i = 0; i < kPieces / 4; ++i) {
+                const int u = i * 64 + lane, t = u / kPieces, c = u % kPieces;
+                const int64_t at = from + t * a.token_stride;
+                load_lds16(kp + at + (c ^ (t & (kPieces - 1))) * 8, lk + i * 512);
+                // behind the end there may be anything, and zero times anything is to be zero
+                const uint16_t *v = vp + at + (c ^ (2 * t & (kPieces - 1))) * 8;
+                load_lds16(t_first + t < end ? v : zeros, lv + i * 512);
+            }
+        };
+        f32x16 o[kDb];
+#pragma unroll
+        for (int i = 0; i < kDb; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[i][r] = 0;
+        float m = kNegInf, l = 0;
+        if (tiles) fetch(0, 0);
+        for (int n = 0; n < tiles; ++n) {
+            wait_loads();
+            __syncthreads();
+            if (n + 1 < tiles) fetch(n + 1, (n + 1) & 1);
+            const uint16_t *lk = lds_k[n & 1], *lv = lds_v[n & 1];
+            f32x16 s[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[h][r] = 0;
+#pragma unroll
+                for (int st = 0; st < kSteps; ++st) {
+                    const int at = (h * 32 + col) * D + (((2 * st + half) ^ (col & (kPieces - 1))) * 8);
+                    s[h] = T::mma32(*reinterpret_cast<const s16x8 *>(lk + at), qf[st], s[h]);
+                }
+            }
+            const int base = it.kv0 + n * kTileKv;
+            if (base + kTileKv > least) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (base + h * 32 + (r >> 2) * 8 + half * 4 + (r & 3) >= lim) s[h][r] = kNegInf;
+            }
+            float top = kNegInf;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[h][r]);
+            top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+            const float now = fmaxf(m, top), use = now == kNegInf ? 0.f : now;
+            if (__any(now != m)) {
+                const float f = exp2_of(m - use);
+                l *= f;
+#pragma unroll
+                for (int i = 0; i < kDb; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[i][r] *= f;
+                m = now;
+            }
+            s16x8 pf[4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[h][r] = exp2_of(fmaf(s[h][r], a.scale_log2, -use));
+                    l += s[h][r];
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    union { uint32_t u[4]; s16x8 v; } w;
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) w.u[y] = T::pack(s[h][8 * x + 2 * y], s[h][8 * x + 2 * y + 1]);
+                    pf[2 * h + x] = w.v;
+                }
+            }
+            const int quad = (lane >> 2) & 3, g16 = (lane >> 4) & 1;
+            const int vt = 4 * half + quad;     // token of this lane's address, within eight
+#pragma unroll
+            for (int i = 0; i < kDb; ++i) {
+                const int piece = (4 * i + 2 * g16 + ((lane & 3) >> 1)) ^ (2 * vt & (kPieces - 1));
+                const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
+#pragma unroll
+                for (int st = 0; st < 4; ++st)
+                    o[i] = T::mma32(join(read_tr(v + st * 16 * D), read_tr(v + (st * 16 + 8) * D)), pf[st], o[i]);
+            }
+        }
+        l += __shfl_xor(l, 32);
+        if (active) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const float lse = l == 0.f ? kNegInf : m + log2_of(l);
+            if (it.part < 0) {
+                uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + hq * a.out_head + 4 * half;
+#pragma unroll
+                for (int i = 0; i < kDb; ++i)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        *reinterpret_cast<uint2 *>(to + 32 * i + 8 * b) =
+                            make_uint2(T::pack(o[i][4 * b] * inv, o[i][4 * b + 1] * inv),
+                                       T::pack(o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv));
+                if (a.lse_out && half == 0) a.lse_out[q_row * a.n_heads + hq] = lse * kLn2;
+            } else {
+                const int64_t at = it.part + (int64_t)tok * a.n_heads + hq;
+                float *to = a.ws.o + at * D + 4 * half;
+#pragma unroll
+                for (int i = 0; i < kDb; ++i)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        *reinterpret_cast<float4 *>(to + 32 * i + 8 * b) =
+                            make_float4(o[i][4 * b] * inv, o[i][4 * b + 1] * inv, o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv);
+                if (half == 0) a.ws.lse[at] = lse;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ narrow items
+
+// Up to 16 rows: a wave by itself, with 16 x 16 x 32 products and 32 tokens
+// (two pages) at a time.  K goes from memory to the registers that multiply it;
+// V through a piece of LDS of the wave's own, for the transposing read.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void attn_narrow(AttnArgs a) {
+    constexpr int kPieces = D / 8, kSteps = D / 32, kDb = D / 16, kTok = 32;
+    __shared__ __align__(1024) uint16_t lds_v[4][kTok * D];
+    if (!a.ws.head->ok) return;
+    const int n_items = a.ws.head->n_narrow;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quarter = lane >> 4;
+    const uint16_t *zeros = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(a.ws.head) + kZeroOffset);
+    const uint16_t *kp = static_cast<const uint16_t *>(a.k), *vp = static_cast<const uint16_t *>(a.v);
+    uint16_t *lv = lds_v[wave];
+    for (int which = blockIdx.x * 4 + wave; which < n_items; which += gridDim.x * 4) {
+        const AttnItem it = a.ws.narrow[which];
+        const int head = it.head_tile & 255;
+        const int tok = col / a.group, hq = head * a.group + col - tok * a.group;
+        const bool active = tok < it.n_tok;
+        const int lim = active ? min(a.ws.lim[it.t0 + tok], it.kv1) : 0;
+        const int64_t q_row = active ? a.ws.tok[it.t0 + tok] : 0;
+        s16x8 qf[kSteps];
+        {
+            const uint16_t *q = static_cast<const uint16_t *>(a.q) + q_row * a.q_token + hq * a.q_head + quarter * 8;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+                qf[s] = active ? *reinterpret_cast<const s16x8 *>(q + 32 * s) : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        }
+        int most = lim;
+#pragma unroll
+        for (int d = 8; d; d >>= 1) most = max(most, __shfl_xor(most, d));
+        const int end = __builtin_amdgcn_readfirstlane(most);
+        const int32_t *table = a.table + (int64_t)it.seq * a.table_width;
+        f32x4 o[kDb];
+#pragma unroll
+        for (int i = 0; i < kDb; ++i) o[i] = f32x4{0, 0, 0, 0};
+        float m = kNegInf, l = 0;
+        for (int base = it.kv0; base < end; base += kTok) {
+            f32x4 s[2];
+            s16x8 kf[2][kSteps];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int t_first = base + h * kBlk;
+                const uint32_t page = min((uint32_t)table[min(t_first, end - 1) / kBlk], (uint32_t)(a.n_pages - 1));
+                const int64_t from = (int64_t)page * a.page_stride + (int64_t)head * a.head_stride;
+                const uint16_t *k = kp + from + col * a.token_stride + quarter * 8;
+#pragma unroll
+                for (int st = 0; st < kSteps; ++st) kf[h][st] = *reinterpret_cast<const s16x8 *>(k + 32 * st);
+#pragma unroll
+                for (int i = 0; i < kPieces / 4; ++i) {
+                    const int u = i * 64 + lane, t = u / kPieces, c = u % kPieces;
+                    const uint16_t *v = vp + from + t * a.token_stride + (c ^ (2 * t & (kPieces - 1))) * 8;
+                    load_lds16(t_first + t < end ? v : zeros, lv + h * kBlk * D + i * 512);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                s[h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int st = 0; st < kSteps; ++st) s[h] = T::mma16(kf[h][st], qf[st], s[h]);
+            }
+            float top = kNegInf;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (base + h * kBlk + quarter * 4 + r >= lim) s[h][r] = kNegInf;
+                    top = fmaxf(top, s[h][r]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+            const float now = fmaxf(m, top), use = now == kNegInf ? 0.f : now;
+            if (__any(now != m)) {
+                const float f = exp2_of(m - use);
+                l *= f;
+#pragma unroll
+                for (int i = 0; i < kDb; ++i) o[i] *= f;
+                m = now;
+            }
+            union { uint32_t u[4]; s16x8 v; } w;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[h][r] = exp2_of(fmaf(s[h][r], a.scale_log2, -use));
+                    l += s[h][r];
+                }
+                w.u[2 * h] = T::pack(s[h][0], s[h][1]);
+                w.u[2 * h + 1] = T::pack(s[h][2], s[h][3]);
+            }
+            wait_loads();
+            const int vt = 4 * quarter + ((lane >> 2) & 3);     // token of this lane's address, within a page
+#pragma unroll
+            for (int i = 0; i < kDb; ++i) {
+                const int piece = (2 * i + ((lane & 3) >> 1)) ^ (2 * vt & (kPieces - 1));
+                const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
+                o[i] = T::mma16(join(read_tr(v), read_tr(v + kBlk * D)), w.v, o[i]);
+            }
+            // the reads are done before the next tokens land in the same place
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (active) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const float lse = l == 0.f ? kNegInf : m + log2_of(l);
+            if (it.part < 0) {
+                uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + hq * a.out_head + 4 * quarter;
+#pragma unroll
+                for (int i = 0; i < kDb; ++i)
+                    *reinterpret_cast<uint2 *>(to + 16 * i) = make_uint2(T::pack(o[i][0] * inv, o[i][1] * inv),
+                                                                         T::pack(o[i][2] * inv, o[i][3] * inv));
+                if (a.lse_out && quarter == 0) a.lse_out[q_row * a.n_heads + hq] = lse * kLn2;
+            } else {
+                const int64_t at = it.part + (int64_t)tok * a.n_heads + hq;
+                float *to = a.ws.o + at * D + 4 * quarter;
+#pragma unroll
+                for (int i = 0; i < kDb; ++i)
+                    *reinterpret_cast<float4 *>(to + 16 * i) =
+                        make_float4(o[i][0] * inv, o[i][1] * inv, o[i][2] * inv, o[i][3] * inv);
+                if (quarter == 0) a.ws.lse[at] = lse;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ join
+
+// A wave for each (query, head): its parts by their sums of exponentials.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_join(AttnArgs a, int32_t n_req) {
+    if (!a.ws.head->ok) return;
+    const int lane = threadIdx.x & 63;
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t t = at / a.n_heads;
+    const int h = (int)(at - t * a.n_heads);
+    if (t >= a.n_tokens) return;
+    const int j = a.ws.pos[t];
+    const AttnParts own = a.ws.parts[j], grp = a.ws.parts[n_req + j];
+    if (own.chunks < 0) return;     // written already
+    const int n = own.chunks + grp.chunks;
+    auto row = [&](int c) -> int64_t {
+        const AttnParts &x = c < grp.chunks ? grp : own;
+        const int k = c < grp.chunks ? c : c - grp.chunks;
+        return x.base + ((int64_t)k * x.n_tok + (t - x.t0)) * a.n_heads + h;
+    };
+    float top = kNegInf;
+    for (int c = lane; c < n; c += 64) top = fmaxf(top, a.ws.lse[row(c)]);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    float sum = 0, o[2] = {0, 0};
+    if (top != kNegInf)
+        for (int c = 0; c < n; ++c) {
+            const int64_t r = row(c);
+            const float lse = a.ws.lse[r];
+            if (lse == kNegInf) continue;
+            const float w = exp2_of(lse - top);
+            sum += w;
+            if (D == 128) {
+                const float2 x = *reinterpret_cast<const float2 *>(a.ws.o + r * D + 2 * lane);
+                o[0] += w * x.x;
+                o[1] += w * x.y;
+            } else {
+                o[0] += w * a.ws.o[r * D + lane];
+            }
+        }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int64_t q_row = a.ws.tok[t];
+    uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + h * a.out_head;
+    if (D == 128) *reinterpret_cast<uint32_t *>(to + 2 * lane) = T::pack(o[0] * inv, o[1] * inv);
+    else to[lane] = (uint16_t)T::pack(o[0] * inv, 0.f);
+    if (a.lse_out && lane == 0) a.lse_out[q_row * a.n_heads + h] = sum == 0.f ? kNegInf : (top + log2_of(sum)) * kLn2;
+}
+
+template <typename T, int D>
+hipError_t launch(const AttnArgs &a, int32_t n_req, hipStream_t st) {
+    attn_wide<T, D><<<512, 256, 0, st>>>(a);
+    attn_narrow<T, D><<<1024, 256, 0, st>>>(a);
+    const int64_t rows = a.n_tokens * a.n_heads;
+    attn_join<T, D><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a, n_req);
+    return hipGetLastError();
+}
+
+int64_t up(int64_t v) { return (v + 255) / 256 * 256; }
+
+}  // namespace
+
+int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, char *base,
+                AttnWs *ws) {
+    // Partial rows: one for every (query, head) of each of its two segments, and
+    // for each item beyond a segment's first of a (tile, KV head) a tile's rows;
+    // of those there are at most as many as the plan aims at.
+    const int64_t rows = 2 * n_tokens * n_heads + (int64_t)kWideRows * kWideItems + (int64_t)kNarrowRows * kNarrowItems;
+    const int64_t q_rows = n_tokens * (n_heads / n_kv_heads);
+    const int64_t wide = n_kv_heads * (2 * (q_rows / kWideRows + 1) + 2LL * n_req) + kWideItems;
+    const int64_t narrow = n_kv_heads * 2LL * n_req + kNarrowItems;
+    if (rows > 0x7fffffff || wide > 0x7fffffff) return -1;
+    int64_t o = 0;
+    auto take = [&](int64_t bytes) { const int64_t at = o; o += up(bytes); return at; };
+    const int64_t head = take(256), tok = take(4 * n_tokens), lim = take(4 * n_tokens), pos = take(4 * n_tokens),
+                  place = take(7 * 4 * (2LL * n_req + 2)), parts = take(3LL * n_req * (int64_t)sizeof(AttnParts)),
+                  w = take(wide * (int64_t)sizeof(AttnItem)), nr = take(narrow * (int64_t)sizeof(AttnItem)),
+                  po = take(rows * head_dim * 4), pl = take(rows * 4);
+    if (ws) {
+        ws->head = reinterpret_cast<AttnHead *>(base + head);
+        ws->tok = reinterpret_cast<int32_t *>(base + tok);
+        ws->lim = reinterpret_cast<int32_t *>(base + lim);
+        ws->pos = reinterpret_cast<int32_t *>(base + pos);
+        ws->place = reinterpret_cast<int32_t *>(base + place);
+        ws->parts = reinterpret_cast<AttnParts *>(base + parts);
+        ws->wide = reinterpret_cast<AttnItem *>(base + w);
+        ws->narrow = reinterpret_cast<AttnItem *>(base + nr);
+        ws->o = reinterpret_cast<float *>(base + po);
+        ws->lse = reinterpret_cast<float *>(base + pl);
+        ws->rows = rows;
+    }
+    return o;
+}
+
+hipError_t launch_attn_plan(const AttnPlanArgs &a, hipStream_t st) {
+    attn_plan<<<1, kPlanThreads, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_attn(const AttnArgs &a, int32_t n_req, int32_t head_dim, int32_t dtype, hipStream_t st) {
+    if (dtype == PC_BF16) return head_dim == 128 ? launch<Bf16, 128>(a, n_req, st) : launch<Bf16, 64>(a, n_req, st);
+    return head_dim == 128 ? launch<Fp16, 128>(a, n_req, st) : launch<Fp16, 64>(a, n_req, st);
+}
+
+}  // namespace pcr

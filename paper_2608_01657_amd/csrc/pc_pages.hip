@@ -1,0 +1,675 @@
+// pc_pages.hip -- pages of a KV cache on gfx950: forking, growing, freeing,
+// compacting and storing, and the groups of a keyed batch.
+//
+// The pool's state is three integer arrays (holders of each page, page tables,
+// lengths).  Every call has a kernel that checks its lists and a kernel that
+// acts, and the second does nothing where the first set the status: a call
+// happens whole or not at all.  Counts change by integer atomics, whose order
+// does not matter; new pages go by rank among the free ones, so results do not
+// depend on timing.
+#include "pc_pages.h"
+
+namespace pcr {
+
+namespace {
+
+constexpr int kThreads = 1024;    // of the kernels that one workgroup runs alone
+
+__device__ __forceinline__ int blocks_of(int tokens) { return (int)(((int64_t)tokens + kBlk - 1) / kBlk); }
+
+__device__ __forceinline__ bool page_ok(const pc_pages &p, int page) { return (uint32_t)page < (uint32_t)p.n_pages; }
+
+__device__ __forceinline__ bool len_ok(const pc_pages &p, int len) {
+    return len >= 0 && (int64_t)len <= (int64_t)p.table_width * kBlk;
+}
+
+// Exclusive sum over the workgroup's threads; *total: over all of them.
+template <typename N>
+__device__ N block_sum(N v, N *total, N *lds) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
+    N x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const N y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 63) lds[w] = x;
+    __syncthreads();
+    N before = 0, all = 0;
+    for (int i = 0; i < nw; ++i) {
+        const N t = lds[i];
+        if (i < w) before += t;
+        all += t;
+    }
+    *total = all;
+    return before + x - v;
+}
+
+// Whether the status was set when the workgroup began: one read for all its
+// threads, for kernels whose workgroups may set it meanwhile.
+__device__ bool stopped(const int32_t *status) {
+    __shared__ int32_t s;
+    if (threadIdx.x == 0) s = __hip_atomic_load(status, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return s != PC_OK;
+}
+
+// Every sequence of the list in the pool, and none twice (seen: a bit for
+// each sequence of the pool).  One workgroup, all of its threads.
+__device__ bool bad_list(const pc_pages &p, const int32_t *seq, int32_t n, uint32_t *seen) {
+    const int words = (p.n_seqs + 31) / 32;
+    for (int i = threadIdx.x; i < words; i += blockDim.x) seen[i] = 0;
+    __syncthreads();
+    bool bad = false;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const uint32_t s = (uint32_t)seq[i];
+        const uint32_t bit = 1u << (s & 31);
+        bad |= s >= (uint32_t)p.n_seqs || (atomicOr(&seen[s >> 5], bit) & bit);
+    }
+    __syncthreads();
+    return bad;
+}
+
+// ------------------------------------------------------------------ copies
+
+// 16 bytes a thread; page_elems is a multiple of 8.
+__device__ __forceinline__ void copy_page(const pc_pages &p, int which, int src, int dst) {
+    const int64_t layer = (int64_t)(which >> 1) * p.layer_stride;
+    uint16_t *base = static_cast<uint16_t *>((which & 1) ? p.d_v : p.d_k) + layer;
+    const uint4 *s = reinterpret_cast<const uint4 *>(base + src * p.page_stride);
+    uint4 *d = reinterpret_cast<uint4 *>(base + dst * p.page_stride);
+    const int n = p.n_kv_heads * p.head_dim * kBlk / 8;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) d[i] = s[i];
+}
+
+// ------------------------------------------------------------------ fork, free
+
+// Workgroup 0 looks at the lists, the others each at one sequence's pages.
+// children == nullptr: the list of pc_pages_free.
+__global__ __launch_bounds__(kThreads) void check_lists(pc_pages p, const int32_t *seq, const int32_t *child, int32_t n,
+                                                        int32_t *status) {
+    if (stopped(status)) return;
+    extern __shared__ uint32_t seen[];
+    bool bad = false;
+    if (blockIdx.x == 0) {
+        bad = bad_list(p, child ? child : seq, n, seen);
+        if (child)
+            for (int i = threadIdx.x; i < n; i += kThreads) {
+                const uint32_t s = (uint32_t)seq[i], c = (uint32_t)child[i];
+                bad |= s >= (uint32_t)p.n_seqs || (seen[s >> 5] >> (s & 31) & 1);
+                bad |= c >= (uint32_t)p.n_seqs || p.d_len[c] != 0;
+            }
+    } else {
+        const uint32_t s = (uint32_t)seq[blockIdx.x - 1];
+        if (s < (uint32_t)p.n_seqs) {
+            const int len = p.d_len[s];
+            if (!len_ok(p, len)) {
+                bad = true;
+            } else {
+                const int32_t *row = p.d_table + (int64_t)s * p.table_width;
+                const int nb = blocks_of(len);
+                for (int i = threadIdx.x; i < nb; i += kThreads) bad |= !page_ok(p, row[i]);
+            }
+        }
+    }
+    if (bad) atomicExch(status, PC_EINVAL);
+}
+
+__global__ __launch_bounds__(256) void fork_pages(pc_pages p, const int32_t *parent, const int32_t *child,
+                                                  const int32_t *status) {
+    if (*status != PC_OK) return;
+    const int64_t from = parent[blockIdx.x], to = child[blockIdx.x];
+    const int len = p.d_len[from], nb = blocks_of(len);
+    const int32_t *src = p.d_table + from * p.table_width;
+    int32_t *dst = p.d_table + to * p.table_width;
+    for (int i = threadIdx.x; i < nb; i += blockDim.x) {
+        const int page = src[i];
+        dst[i] = page;
+        atomicAdd(&p.d_refs[page], 1);
+    }
+    if (threadIdx.x == 0) p.d_len[to] = len;
+}
+
+__global__ __launch_bounds__(256) void free_pages(pc_pages p, const int32_t *seq, const int32_t *status) {
+    if (*status != PC_OK) return;
+    const int64_t s = seq[blockIdx.x];
+    const int nb = blocks_of(p.d_len[s]);
+    const int32_t *row = p.d_table + s * p.table_width;
+    for (int i = threadIdx.x; i < nb; i += blockDim.x) atomicSub(&p.d_refs[row[i]], 1);
+    __syncthreads();
+    if (threadIdx.x == 0) p.d_len[s] = 0;
+}
+
+// ------------------------------------------------------------------ free pages
+
+// Bitmap and count of a chunk's free pages.
+__global__ __launch_bounds__(256) void scan_refs(pc_pages p, PagesWs ws, const int32_t *status) {
+    if (*status != PC_OK) return;
+    __shared__ int32_t sums[4];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int base = blockIdx.x * kChunkPages + w * (kChunkPages / 4);
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < kChunkPages / 256; ++i) {
+        const int page = base + i * 64 + lane;
+        const uint64_t m = __ballot(page < p.n_pages && p.d_refs[page] == 0);
+        if (lane == 0) ws.free_bits[base / 64 + i] = m;
+        count += __popcll(m);
+    }
+    if (lane == 0) sums[w] = count;
+    __syncthreads();
+    if (threadIdx.x == 0) ws.chunk_free[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+}
+
+// Free pages of all chunks; chunk_free becomes those before the chunk.  One
+// workgroup, all of its threads.
+__device__ int sum_chunks(const PagesWs &ws, int *lds) {
+    int before = 0;
+    for (int c0 = 0; c0 < ws.n_chunks; c0 += kThreads) {
+        const int c = c0 + threadIdx.x;
+        const int v = c < ws.n_chunks ? ws.chunk_free[c] : 0;
+        int all;
+        const int x = block_sum(v, &all, lds);
+        if (c < ws.n_chunks) ws.chunk_free[c] = before + x;
+        before += all;
+    }
+    return before;
+}
+
+// ------------------------------------------------------------------ extend
+
+// One workgroup: checks the list, says which last pages are copied, gives
+// every sequence its ranks among the free pages, and takes the copied pages'
+// holders off them.  A shared last page's count tells whether all its holders
+// grow: each takes itself off, and where nothing is left the lowest place in
+// the list, found by an atomic minimum in the same word, keeps the page.
+__global__ __launch_bounds__(kThreads) void extend_plan(pc_pages p, const int32_t *seq, const int32_t *add, int32_t n,
+                                                        PagesWs ws, int32_t *status) {
+    if (*status != PC_OK) return;
+    extern __shared__ uint32_t seen[];
+    __shared__ int lds[16];
+    __shared__ int64_t lds64[16];
+    __shared__ int any_bad;
+    int32_t *first = ws.entry, *have = first + n, *fresh = have + n, *copied = fresh + n;
+    const int words = (p.n_seqs + 31) / 32;
+    for (int i = threadIdx.x; i < words; i += kThreads) seen[i] = 0;
+    if (threadIdx.x == 0) {
+        any_bad = 0;
+        ws.head[0] = 0;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const uint32_t s = (uint32_t)seq[i];
+        const int a = add[i];
+        bool bad = s >= (uint32_t)p.n_seqs || a < 0;
+        int src = -1, nb = 0, more = 0;
+        if (!bad) {
+            const uint32_t bit = 1u << (s & 31);
+            const int len = p.d_len[s];
+            bad = (atomicOr(&seen[s >> 5], bit) & bit) || !len_ok(p, len) ||
+                  (int64_t)len + a > (int64_t)p.table_width * kBlk;
+            if (!bad) {
+                nb = blocks_of(len);
+                more = blocks_of(len + a) - nb;
+                if (a > 0 && len % kBlk) {
+                    const int page = p.d_table[(int64_t)s * p.table_width + nb - 1];
+                    if (!page_ok(p, page)) bad = true;
+                    else if (p.d_refs[page] > 1) src = page;
+                }
+            }
+        }
+        have[i] = nb;
+        fresh[i] = more;
+        copied[i] = src;
+        if (bad) any_bad = 1;
+    }
+    __syncthreads();
+    if (any_bad) {
+        if (threadIdx.x == 0) *status = PC_EINVAL;
+        return;
+    }
+    for (int i = threadIdx.x; i < n; i += kThreads)
+        if (copied[i] >= 0) atomicSub(&p.d_refs[copied[i]], 1);
+    __threadfence();
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kThreads)
+        if (copied[i] >= 0 &&
+            __hip_atomic_load(&p.d_refs[copied[i]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) <= 0)
+            atomicMin(&p.d_refs[copied[i]], i - n);
+    __threadfence();
+    __syncthreads();
+    int64_t total = 0;
+    for (int i0 = 0; i0 < n; i0 += kThreads) {
+        const int i = i0 + threadIdx.x;
+        int need = 0;
+        if (i < n) {
+            need = fresh[i];
+            if (copied[i] >= 0) {
+                const int at = __hip_atomic_load(&p.d_refs[copied[i]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (at == i - n) copied[i] = -2 - copied[i];    // keeps it
+                else ++need;
+            }
+        }
+        int64_t all;
+        const int64_t x = block_sum((int64_t)need, &all, lds64);
+        if (i < n) {
+            first[i] = (int32_t)(total + x);    // of use only where the pool has them all
+            fresh[i] = need;
+        }
+        total += all;
+    }
+    const bool short_of = total > sum_chunks(ws, lds);
+    __syncthreads();
+    // the counts: kept pages have one holder again; where the pool is short, all as before
+    for (int i = threadIdx.x; i < n; i += kThreads)
+        if (copied[i] <= -2)
+            __hip_atomic_store(&p.d_refs[-2 - copied[i]], short_of ? 0 : 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __threadfence();
+    __syncthreads();
+    if (short_of) {
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            if (copied[i] == -1) continue;
+            atomicAdd(&p.d_refs[copied[i] <= -2 ? -2 - copied[i] : copied[i]], 1);
+        }
+        if (threadIdx.x == 0) *status = PC_ENOPAGES;
+    } else if (threadIdx.x == 0) {
+        ws.head[0] = (int32_t)total;
+    }
+}
+
+// The free pages of rank < head[0], listed by rank; they have a holder now.
+__global__ __launch_bounds__(256) void list_free(pc_pages p, PagesWs ws, const int32_t *status) {
+    if (*status != PC_OK) return;
+    __shared__ int lds[4];
+    const int total = ws.head[0];
+    const int before = ws.chunk_free[blockIdx.x];
+    if (before >= total) return;
+    const int t = threadIdx.x;
+    const uint64_t m = t < 64 ? ws.free_bits[(int64_t)blockIdx.x * 64 + t] : 0;
+    int all;
+    int rank = before + block_sum((int)__popcll(m), &all, lds);
+    const int base = blockIdx.x * kChunkPages + t * 64;
+    for (uint64_t x = m; x && rank < total; x &= x - 1, ++rank) {
+        const int page = base + __ffsll((unsigned long long)x) - 1;
+        ws.list[rank] = page;
+        p.d_refs[page] = 1;
+    }
+}
+
+__global__ __launch_bounds__(256) void extend_pages(pc_pages p, const int32_t *seq, const int32_t *add, int32_t n,
+                                                    PagesWs ws, const int32_t *status) {
+    if (*status != PC_OK) return;
+    const int i = blockIdx.x;
+    const int first = ws.entry[i], have = ws.entry[n + i], fresh = ws.entry[2 * n + i], src = ws.entry[3 * n + i];
+    if (blockIdx.y == 0) {
+        const int64_t s = seq[i];
+        int32_t *row = p.d_table + s * p.table_width + have - (src >= 0);
+        for (int j = threadIdx.x; j < fresh; j += blockDim.x) row[j] = ws.list[first + j];
+        if (threadIdx.x == 0) p.d_len[s] += add[i];
+    }
+    if (src >= 0) copy_page(p, blockIdx.y, src, ws.list[first]);
+}
+
+// ------------------------------------------------------------------ compact
+
+// One workgroup: pages in use, and how many of them lie behind that number.
+__global__ __launch_bounds__(kThreads) void compact_plan(pc_pages p, PagesWs ws, int32_t *n_live, const int32_t *status) {
+    if (*status != PC_OK) {
+        if (threadIdx.x == 0) ws.head[3] = 0;
+        return;
+    }
+    __shared__ int lds[16];
+    const int live = p.n_pages - sum_chunks(ws, lds);
+    __syncthreads();
+    int holes = 0;
+    if (live < p.n_pages) {
+        // free pages before page `live`
+        const int c = live / kChunkPages, in = live % kChunkPages, t = threadIdx.x;
+        int x = 0;
+        if (t < 64 && t * 64 < in) {
+            const uint64_t m = ws.free_bits[(int64_t)c * 64 + t];
+            const int bits = in - t * 64;
+            x = __popcll(bits >= 64 ? m : m & ((1ull << bits) - 1));
+        }
+        int all;
+        block_sum(x, &all, lds);
+        holes = ws.chunk_free[c] + all;
+    }
+    if (threadIdx.x == 0) {
+        ws.head[0] = live;
+        ws.head[1] = holes;
+        ws.head[3] = 1;
+        *n_live = live;
+    }
+}
+
+// Rank by rank: the free places before n_live, and the pages behind it.
+__global__ __launch_bounds__(256) void list_moves(pc_pages p, PagesWs ws, const int32_t *status) {
+    if (*status != PC_OK) return;
+    __shared__ int lds[4];
+    const int live = ws.head[0], holes = ws.head[1], t = threadIdx.x;
+    const uint64_t m = t < 64 ? ws.free_bits[(int64_t)blockIdx.x * 64 + t] : 0;
+    const int base = blockIdx.x * kChunkPages + t * 64;
+    int all;
+    const int free_before = ws.chunk_free[blockIdx.x] + block_sum((int)__popcll(m), &all, lds);
+    if (t >= 64 || base >= p.n_pages) return;
+    int rank = free_before;
+    for (uint64_t x = m; x && rank < holes; x &= x - 1, ++rank)
+        ws.list[rank] = base + __ffsll((unsigned long long)x) - 1;
+    const int bits = p.n_pages - base;
+    uint64_t used = ~m;
+    if (bits < 64) used &= (1ull << bits) - 1;
+    // pages in use before this word, less those that stay
+    int moves = base - free_before - (live - holes);
+    for (; used; used &= used - 1) {
+        const int page = base + __ffsll((unsigned long long)used) - 1;
+        if (page >= live) {
+            ws.moved[moves] = page;
+            ws.rank[page] = moves;
+        }
+        ++moves;
+    }
+}
+
+__global__ __launch_bounds__(256) void compact_pages(pc_pages p, int32_t *refs_to, int32_t *table_to, PagesWs ws,
+                                                     int32_t *status) {
+    if (ws.head[3] == 0) return;    // the status that compact_plan saw; this kernel sets it itself
+    const int live = ws.head[0], moves = ws.head[1];
+    const int64_t copies = (int64_t)moves * 2 * p.n_layers;
+    for (int64_t u = blockIdx.x; u < copies; u += gridDim.x) {
+        const int which = (int)(u / moves), i = (int)(u - (int64_t)which * moves);
+        copy_page(p, which, ws.moved[i], ws.list[i]);
+    }
+    const int64_t step = (int64_t)gridDim.x * blockDim.x, at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    auto is_free = [&](int page) { return ws.free_bits[page >> 6] >> (page & 63) & 1; };
+    for (int64_t u = at; u < p.n_pages; u += step) {
+        const int page = (int)u;
+        if (page < live) {
+            if (!is_free(page)) refs_to[page] = p.d_refs[page];
+        } else if (is_free(page)) {
+            refs_to[page] = 0;
+        } else {    // both counts of a move by one thread: the two arrays may be one
+            refs_to[ws.list[ws.rank[page]]] = p.d_refs[page];
+            refs_to[page] = 0;
+        }
+    }
+    const int64_t entries = (int64_t)p.n_seqs * p.table_width;
+    bool bad = false;
+    for (int64_t u = at; u < entries; u += step) {
+        const int64_t s = u / p.table_width;
+        int page = p.d_table[u];
+        const int len = p.d_len[s];
+        if (!len_ok(p, len)) {
+            bad = true;
+        } else if (u - s * p.table_width < blocks_of(len)) {
+            if (!page_ok(p, page) || is_free(page)) bad = true;
+            else if (page >= live) page = ws.list[ws.rank[page]];
+        }
+        table_to[u] = page;
+    }
+    if (bad) atomicExch(status, PC_EINVAL);
+}
+
+// ------------------------------------------------------------------ write
+
+__global__ __launch_bounds__(256) void write_rows(pc_pages p, int32_t layer, const int32_t *seq, const int32_t *new_off,
+                                                  int32_t n, int64_t n_tokens, pc_rows kn, pc_rows vn, int32_t *status) {
+    if (stopped(status)) return;
+    extern __shared__ uint32_t seen[];
+    bool bad = false;
+    const int i = blockIdx.x;
+    if (i == n) {    // the last column looks at the list
+        if (blockIdx.y == 0 && bad_list(p, seq, n, seen)) atomicExch(status, PC_EINVAL);
+        return;
+    }
+    const uint32_t s = (uint32_t)seq[i];
+    const int64_t r0 = new_off[i], r1 = new_off[i + 1];
+    const int len = s < (uint32_t)p.n_seqs ? p.d_len[s] : -1;
+    if (r0 < 0 || r1 < r0 || r1 > n_tokens || !len_ok(p, len) || r1 - r0 > len) {
+        bad = true;
+    } else {
+        const int32_t *row = p.d_table + (int64_t)s * p.table_width;
+        const int per_row = p.head_dim / 8, units = p.n_kv_heads * per_row;
+        const int64_t layer_off = (int64_t)layer * p.layer_stride;
+        const int32_t head_stride = p.layout == PC_HEADS_FIRST ? kBlk * p.head_dim : p.head_dim;
+        const int32_t token_stride = p.layout == PC_HEADS_FIRST ? p.head_dim : p.n_kv_heads * p.head_dim;
+        const int64_t all = (r1 - r0) * units;
+        for (int64_t u = (int64_t)blockIdx.y * blockDim.x + threadIdx.x; u < all; u += (int64_t)gridDim.y * blockDim.x) {
+            const int64_t j = u / units;
+            const int w = (int)(u - j * units), h = w / per_row, c = w - h * per_row;
+            const int pos = (int)(len - (r1 - r0) + j);
+            const int page = row[pos / kBlk];
+            if (!page_ok(p, page) || p.d_refs[page] != 1) {
+                bad = true;
+                continue;
+            }
+            const int64_t to = layer_off + page * p.page_stride + (pos % kBlk) * token_stride + h * head_stride + c * 8;
+            const int64_t kf = (r0 + j) * kn.token_stride + h * kn.head_stride + c * 8;
+            const int64_t vf = (r0 + j) * vn.token_stride + h * vn.head_stride + c * 8;
+            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.d_k) + to) =
+                *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(kn.d_data) + kf);
+            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.d_v) + to) =
+                *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(vn.d_data) + vf);
+        }
+    }
+    if (bad) atomicExch(status, PC_EINVAL);
+}
+
+// ------------------------------------------------------------------ groups
+
+// One workgroup: the first request with the same key of block min_blocks - 1
+// by a hash table in LDS, then a sort by (that request, own number).  Leaves
+// each request's group beside its number in d_order for the next kernel, and
+// the first request's blocks in d_shared.
+__global__ __launch_bounds__(kThreads) void group_requests(const uint64_t *keys, int64_t n_keys, const int64_t *key_off,
+                                                           int32_t R, int32_t Rp, int32_t min_blocks, int32_t *order,
+                                                           int32_t *group_off, int32_t *shared, int32_t *n_groups,
+                                                           int32_t *status) {
+    if (*status != PC_OK) return;
+    extern __shared__ __align__(16) uint64_t mark[];          // [Rp]
+    int32_t *lead = reinterpret_cast<int32_t *>(mark + Rp);   // [Rp] then the sorted words
+    int32_t *tab = lead + Rp;                                 // [2 Rp]
+    __shared__ int lds[16];
+    __shared__ int any_bad;
+    if (threadIdx.x == 0) any_bad = 0;
+    for (int i = threadIdx.x; i < 2 * Rp; i += kThreads) tab[i] = -1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < Rp; i += kThreads) {
+        lead[i] = i;
+        if (i < R) {
+            const int64_t a = key_off[i], b = key_off[i + 1];
+            if (a < 0 || b < a || b > n_keys || b - a > (1 << 26)) any_bad = 1;
+            else if (b - a >= min_blocks) mark[i] = keys[a + min_blocks - 1];
+        }
+    }
+    __syncthreads();
+    if (any_bad) {
+        if (threadIdx.x == 0) *status = PC_EINVAL;
+        return;
+    }
+    constexpr int kPer = PC_MAX_BATCH / kThreads;
+    int rep[kPer];
+    const uint32_t slots = 2 * Rp;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int i = e * kThreads + threadIdx.x;
+        rep[e] = i;
+        if (i >= R || key_off[i + 1] - key_off[i] < min_blocks) continue;
+        uint32_t at = (uint32_t)((mark[i] * 0x9E3779B97F4A7C15ull) >> 40) & (slots - 1);
+        for (;;) {      // at most half of the slots are ever taken
+            const int cur = atomicCAS(&tab[at], -1, i);
+            if (cur < 0) break;
+            if (mark[cur] == mark[i]) {
+                rep[e] = cur;
+                atomicMin(&lead[cur], i);
+                break;
+            }
+            at = (at + 1) & (slots - 1);
+        }
+    }
+    __syncthreads();
+    int word[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int i = e * kThreads + threadIdx.x;
+        word[e] = i < R ? lead[rep[e]] * PC_MAX_BATCH + i : 0x7fffffff;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int i = e * kThreads + threadIdx.x;
+        if (i < Rp) lead[i] = word[e];
+    }
+    __syncthreads();
+    for (int k = 2; k <= Rp; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            for (int t = threadIdx.x; t < Rp / 2; t += kThreads) {
+                const int a = (t / j) * 2 * j + t % j, b = a + j;
+                const int x = lead[a], y = lead[b];
+                if ((x > y) == ((a & k) == 0)) {
+                    lead[a] = y;
+                    lead[b] = x;
+                }
+            }
+            __syncthreads();
+        }
+    int groups = 0;
+    for (int p0 = 0; p0 < R; p0 += kThreads) {
+        const int q = p0 + threadIdx.x;
+        const int x = q < R ? lead[q] : 0;
+        const int l = x / PC_MAX_BATCH, i = x % PC_MAX_BATCH;
+        const bool begins = q < R && (q == 0 || lead[q - 1] / PC_MAX_BATCH != l);
+        int all;
+        const int g = groups + block_sum((int)begins, &all, lds) + begins - 1;
+        if (q < R) order[q] = g * PC_MAX_BATCH + i;
+        if (begins) {
+            const bool alone = q + 1 >= R || lead[q + 1] / PC_MAX_BATCH != l;
+            group_off[g] = q;
+            shared[g] = alone ? 0 : (int32_t)(key_off[i + 1] - key_off[i]);
+        }
+        groups += all;
+    }
+    for (int g = groups + threadIdx.x; g <= R; g += kThreads) {
+        group_off[g] = R;
+        if (g < R) shared[g] = 0;
+    }
+    if (threadIdx.x == 0) *n_groups = groups;
+}
+
+// A workgroup for each request: how many leading keys it has in common with
+// its group's first one.
+__global__ __launch_bounds__(256) void group_shared(const uint64_t *keys, const int64_t *key_off, int32_t *order,
+                                                    const int32_t *group_off, int32_t *shared,
+                                                    const int32_t *status) {
+    if (*status != PC_OK) return;
+    __shared__ int first_off;
+    const int q = blockIdx.x;
+    const int x = order[q], g = x / PC_MAX_BATCH, i = x % PC_MAX_BATCH;
+    const int q0 = group_off[g];
+    if (q > q0) {
+        // the word of the group's first request may be the number alone already
+        const int l = __hip_atomic_load(&order[q0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) % PC_MAX_BATCH;
+        const int64_t a = key_off[i], b = key_off[l];
+        const int64_t na = key_off[i + 1] - a, nb = key_off[l + 1] - b;
+        const int n = (int)(na < nb ? na : nb);
+        if (threadIdx.x == 0) first_off = n;
+        __syncthreads();
+        for (int k0 = 0; k0 < n; k0 += 1024) {
+            int off = 0x7fffffff;
+#pragma unroll
+            for (int e = 3; e >= 0; --e) {
+                const int k = k0 + e * 256 + threadIdx.x;
+                if (k < n && keys[a + k] != keys[b + k]) off = k;
+            }
+            if (off < n) atomicMin(&first_off, off);
+            __syncthreads();
+            const int found = first_off;
+            __syncthreads();
+            if (found < n) break;
+        }
+        if (threadIdx.x == 0) atomicMin(&shared[g], first_off);
+    }
+    if (threadIdx.x == 0) __hip_atomic_store(&order[q], i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+int64_t up(int64_t v) { return (v + 255) / 256 * 256; }
+
+}  // namespace
+
+int64_t pages_ws(const pc_pages &p, int64_t n, char *base, PagesWs *ws) {
+    const int32_t chunks = (p.n_pages + kChunkPages - 1) / kChunkPages;
+    int64_t o = 0;
+    auto take = [&](int64_t bytes) { const int64_t at = o; o += up(bytes); return at; };
+    const int64_t bits = take((int64_t)chunks * 512), cf = take(4LL * chunks), list = take(4LL * p.n_pages),
+                  moved = take(4LL * p.n_pages), rank = take(4LL * p.n_pages), entry = take(16 * (n < 1 ? 1 : n)),
+                  head = take(16);
+    if (ws)
+        *ws = PagesWs{reinterpret_cast<uint64_t *>(base + bits), reinterpret_cast<int32_t *>(base + cf),
+                      reinterpret_cast<int32_t *>(base + list), reinterpret_cast<int32_t *>(base + moved),
+                      reinterpret_cast<int32_t *>(base + rank), reinterpret_cast<int32_t *>(base + entry),
+                      reinterpret_cast<int32_t *>(base + head), chunks};
+    return o;
+}
+
+static size_t seen_bytes(const pc_pages &p) { return (size_t)((p.n_seqs + 31) / 32) * 4; }
+
+hipError_t launch_fork(const pc_pages &p, const int32_t *parent, const int32_t *child, int32_t n, int32_t *status,
+                       hipStream_t st) {
+    check_lists<<<n + 1, kThreads, seen_bytes(p), st>>>(p, parent, child, n, status);
+    fork_pages<<<n, 256, 0, st>>>(p, parent, child, status);
+    return hipGetLastError();
+}
+
+hipError_t launch_free(const pc_pages &p, const int32_t *seq, int32_t n, int32_t *status, hipStream_t st) {
+    check_lists<<<n + 1, kThreads, seen_bytes(p), st>>>(p, seq, nullptr, n, status);
+    free_pages<<<n, 256, 0, st>>>(p, seq, status);
+    return hipGetLastError();
+}
+
+hipError_t launch_extend(const pc_pages &p, const int32_t *seq, const int32_t *add, int32_t n, const PagesWs &ws,
+                         int32_t *status, hipStream_t st) {
+    scan_refs<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+    extend_plan<<<1, kThreads, seen_bytes(p), st>>>(p, seq, add, n, ws, status);
+    list_free<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+    extend_pages<<<dim3(n, 2 * p.n_layers), 256, 0, st>>>(p, seq, add, n, ws, status);
+    return hipGetLastError();
+}
+
+hipError_t launch_compact(const pc_pages &p, int32_t *refs_to, int32_t *table_to, int32_t *n_live, const PagesWs &ws,
+                          int32_t *status, hipStream_t st) {
+    scan_refs<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+    compact_plan<<<1, kThreads, 0, st>>>(p, ws, n_live, status);
+    list_moves<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+    compact_pages<<<2048, 256, 0, st>>>(p, refs_to, table_to, ws, status);
+    return hipGetLastError();
+}
+
+hipError_t launch_write(const pc_pages &p, int32_t layer, const int32_t *seq, const int32_t *new_off, int32_t n,
+                        int64_t n_tokens, const pc_rows &k_new, const pc_rows &v_new, int32_t *status, hipStream_t st) {
+    // workgroups enough for the case that one sequence has all the tokens, but not over 4096 in all
+    int64_t y = (n_tokens * p.n_kv_heads * (p.head_dim / 8) + 1023) / 1024;
+    const int64_t most = 4096 / n > 1 ? 4096 / n : 1;
+    y = y < 1 ? 1 : y > most ? most : y;
+    write_rows<<<dim3(n + 1, (uint32_t)y), 256, seen_bytes(p), st>>>(p, layer, seq, new_off, n, n_tokens, k_new, v_new, status);
+    return hipGetLastError();
+}
+
+hipError_t launch_groups(const uint64_t *keys, int64_t n_keys, const int64_t *key_off, int32_t n_req,
+                         int32_t min_blocks, int32_t *order, int32_t *group_off, int32_t *shared, int32_t *n_groups,
+                         int32_t *status, hipStream_t st) {
+    int32_t rp = 2;
+    while (rp < n_req) rp <<= 1;
+    const size_t bytes = (size_t)rp * (8 + 4 + 8);
+    if (bytes > 64 * 1024 - 256) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&group_requests),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e != hipSuccess) return e;
+    }
+    group_requests<<<1, kThreads, bytes, st>>>(keys, n_keys, key_off, n_req, rp, min_blocks, order, group_off, shared,
+                                               n_groups, status);
+    group_shared<<<n_req, 256, 0, st>>>(keys, key_off, order, group_off, shared, status);
+    return hipGetLastError();
+}
+
+}  // namespace pcr

@@ -1,17 +1,24 @@
 """Device-side driver of the hot path: upload a trace, cut and hash it, replay
-a batch of instances.  Only allocation and argument marshalling happen here;
-all work runs in libpcreplay's kernels on the current HIP stream."""
+a batch of instances; and of the cache itself: pages of K and V (PagePool), the
+groups of a keyed batch (prefix_groups) and attention that reads a group's
+shared prefix once (PrefixBatch).  Only allocation and argument marshalling
+happen here; all work runs in libpcreplay's kernels on the current HIP stream
+of the tensors' device, or the one given."""
 from __future__ import annotations
 
+import contextlib
+import math
 from dataclasses import dataclass
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
 
-from . import (make_instance_desc, phase_counters, make_trace_desc, pc_block_offsets, pc_get_stats, pc_hash_blocks,
-               pc_replay_batch, pc_replay_route_offset, pc_replay_workspace_bytes, pc_replay_workspace_min_bytes,
-               stats_to_dicts, PC_ROUTE_GENERAL, PC_STATS_RECORD_BYTES)
+from . import (make_instance_desc, make_pages, make_rows, phase_counters, make_trace_desc, pc_attn, pc_attn_plan,
+               pc_attn_workspace_bytes, pc_block_offsets, pc_get_stats, pc_hash_blocks, pc_pages_compact,
+               pc_pages_extend, pc_pages_fork, pc_pages_free, pc_pages_workspace_bytes, pc_pages_write,
+               pc_prefix_groups, pc_replay_batch, pc_replay_route_offset, pc_replay_workspace_bytes, pc_replay_workspace_min_bytes,
+               stats_to_dicts, PC_BLOCK_TOKENS, PC_ROUTE_GENERAL, PC_STATS_RECORD_BYTES)
 
 
 @dataclass
@@ -248,3 +255,202 @@ class TraceSet:
         """Key offsets of trace j relative to its own first key (host copy)."""
         o = self.dt.key_off[int(self.req_base[j]):int(self.req_base[j + 1]) + 1].cpu().numpy()
         return o - o[0]
+
+
+# ---------------------------------------------------------------------------
+# Pages of K and V, and attention over them
+# ---------------------------------------------------------------------------
+
+def _need(ok, message):
+    if not ok:
+        raise ValueError(message)
+
+
+def _list(x, dev, what, dtype=torch.int32):
+    _need(x.dtype == dtype and x.device == dev and x.dim() == 1 and x.is_contiguous(),
+          f"{what}: a contiguous one-dimensional {dtype} tensor on {dev}")
+    return x
+
+
+@contextlib.contextmanager
+def _other(dev, stream):
+    """`dev` is the current device, and `stream` the one that new tensors belong to."""
+    with torch.cuda.device(dev):
+        if isinstance(stream, torch.cuda.Stream):
+            with torch.cuda.stream(stream):
+                yield
+        else:
+            yield
+
+
+_here = contextlib.nullcontext()
+
+
+def _on(dev, stream):
+    return _here if stream is None and torch.cuda.current_device() == dev.index else _other(dev, stream)
+
+
+class PagePool:
+    """The pages of a KV cache and the sequences that hold them: 16 tokens a
+    page, K and V [layers, pages, heads, 16, dim], or [layers, pages, 16,
+    heads, dim] with tokens_first; the layers and pages may be strided, a page
+    is contiguous.  Sequences have numbers 0 .. n_seqs-1.
+
+    The arrays are the pool's: `table` [n_seqs, table_width], `length` and
+    `refs` [pages] (holders), all int32; made empty unless given.  `status`
+    collects what the calls find wrong on the device (PC_EINVAL, PC_ENOPAGES):
+    once it is set, further calls do nothing until it is zeroed.  Every call
+    is asynchronous and can be captured into a graph."""
+
+    def __init__(self, k, v, n_seqs: Optional[int] = None, table_width: Optional[int] = None, table=None, length=None,
+                 refs=None, tokens_first: bool = False):
+        _need(k.dim() == 5 and k.shape == v.shape and k.dtype == v.dtype and k.device == v.device
+              and k.stride() == v.stride(), "k and v: [layers, pages, .., .., dim], alike in shape, type and strides")
+        _need(k.is_cuda, "k and v: on a GPU")
+        _need(k.dtype in (torch.bfloat16, torch.float16), f"k and v: bfloat16 or float16, not {k.dtype}")
+        _need(k.shape[2 if tokens_first else 3] == PC_BLOCK_TOKENS, f"a page has {PC_BLOCK_TOKENS} tokens")
+        _need(k[0, 0].is_contiguous(), "a page is contiguous")
+        dev = self.device = k.device
+        self.k, self.v, self.tokens_first = k, v, tokens_first
+        if table is None:
+            _need(n_seqs is not None and table_width is not None, "n_seqs and table_width, or table")
+            table = torch.full((n_seqs, table_width), -1, dtype=torch.int32, device=dev)
+        _need(table.dim() == 2 and table.is_contiguous() and table.dtype == torch.int32 and table.device == dev,
+              f"table: a contiguous int32 matrix on {dev}")
+        zeros = lambda n: torch.zeros(n, dtype=torch.int32, device=dev)
+        self.table = table
+        self.length = _list(zeros(table.shape[0]) if length is None else length, dev, "length")
+        self.refs = _list(zeros(k.shape[1]) if refs is None else refs, dev, "refs")
+        _need(self.length.numel() == table.shape[0], "length: one for each row of the table")
+        _need(self.refs.numel() == k.shape[1], "refs: one for each page")
+        self.status = zeros(1)
+        self.desc = make_pages(k, v, self.refs, self.table, self.length, tokens_first)
+        n = pc_pages_workspace_bytes(self.desc, table.shape[0])
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)
+
+    @property
+    def n_heads(self) -> int:
+        return self.desc.n_kv_heads
+
+    def fork(self, parent, child, stream=None):
+        """Sequences child[i], empty, take over parent[i]'s pages and length."""
+        _need(parent.numel() == child.numel(), "as many parents as children")
+        with _on(self.device, stream):
+            pc_pages_fork(self.desc, _list(parent, self.device, "parent"), _list(child, self.device, "child"),
+                          self.status, stream)
+
+    def extend(self, seq, add, stream=None):
+        """Sequences seq[i] grow by add[i] tokens: new pages, and a copy of a
+        last page that others hold too."""
+        _need(seq.numel() == add.numel(), "a length for each sequence")
+        with _on(self.device, stream):
+            pc_pages_extend(self.desc, _list(seq, self.device, "seq"), _list(add, self.device, "add"), self.workspace,
+                            self.status, stream)
+
+    def free(self, seq, stream=None):
+        """Sequences seq[i] give up their pages and are empty."""
+        with _on(self.device, stream):
+            pc_pages_free(self.desc, _list(seq, self.device, "seq"), self.status, stream)
+
+    def compact(self, refs_to=None, table_to=None, stream=None):
+        """Pages in use move to the lowest numbers; counts and tables are
+        rewritten in place, or to refs_to and table_to.  Returns the number of
+        pages in use (a tensor)."""
+        refs_to = self.refs if refs_to is None else _list(refs_to, self.device, "refs_to")
+        table_to = self.table if table_to is None else table_to
+        _need(refs_to.numel() == self.refs.numel(), "refs_to: one for each page")
+        _need(table_to.shape == self.table.shape and table_to.is_contiguous() and table_to.dtype == torch.int32
+              and table_to.device == self.device, "table_to: like the table")
+        with _on(self.device, stream):
+            n_live = torch.empty(1, dtype=torch.int32, device=self.device)
+            pc_pages_compact(self.desc, refs_to, table_to, n_live, self.workspace, self.status, stream)
+        return n_live
+
+    def write(self, layer: int, seq, new_off, k_new, v_new, stream=None):
+        """Rows new_off[i] .. new_off[i+1]-1 of k_new and v_new [tokens, heads,
+        dim] become K and V of sequence seq[i]'s last tokens."""
+        for x in (k_new, v_new):
+            self._rows(x, self.desc.n_kv_heads, "k_new and v_new")
+        _need(k_new.shape == v_new.shape, "k_new and v_new are alike")
+        _need(new_off.numel() == seq.numel() + 1, "new_off: one more than sequences")
+        with _on(self.device, stream):
+            pc_pages_write(self.desc, layer, _list(seq, self.device, "seq"), _list(new_off, self.device, "new_off"),
+                           k_new.shape[0], make_rows(k_new), make_rows(v_new), self.status, stream)
+
+    def _rows(self, x, heads, what):
+        d = self.desc
+        _need(x.dim() == 3 and x.shape[1] == heads and x.shape[2] == d.head_dim and x.dtype == self.k.dtype
+              and x.device == self.device and (x.stride(2) == 1 or x.numel() == 0),
+              f"{what}: [tokens, {heads}, {d.head_dim}] of {self.k.dtype} on {self.device}, the last dimension contiguous")
+
+
+class PrefixGroups(NamedTuple):
+    """A batch in groups that share leading blocks (see pc_prefix_groups)."""
+    order: torch.Tensor         # int32 [R] requests, group by group
+    group_off: torch.Tensor     # int32 [R+1] where each group begins; R behind the last
+    shared: torch.Tensor        # int32 [R] blocks that a group's requests share
+    n_groups: torch.Tensor      # int32 [1]
+    status: torch.Tensor        # int32 [1]
+
+
+def prefix_groups(keys, key_off, min_blocks: int = 1, stream=None) -> PrefixGroups:
+    """Groups of the requests whose block keys (cut_and_hash: keys, key_off)
+    are alike for min_blocks blocks or more, and how many leading blocks each
+    group shares."""
+    dev = key_off.device
+    _need(dev.type == "cuda", "keys and key_off: on a GPU")
+    _list(key_off, dev, "key_off", torch.int64)
+    _list(keys, dev, "keys", torch.int64)
+    R = key_off.numel() - 1
+    _need(R >= 1, "key_off: n_req + 1 offsets")
+    with _on(dev, stream):
+        g = PrefixGroups(*torch.zeros(3 * R + 3, dtype=torch.int32, device=dev).split((R, R + 1, R, 1, 1)))
+        pc_prefix_groups(keys, key_off, min_blocks, *g, stream)
+    return g
+
+
+class PrefixBatch:
+    """Attention of a batch over a PagePool: n_req requests with n_tokens
+    queries in all, of n_heads heads.  plan() once for the lengths that the
+    sequences then have, attend() for every layer."""
+
+    def __init__(self, pool: PagePool, n_req: int, n_tokens: int, n_heads: int):
+        self.pool, self.n_req, self.n_tokens, self.n_heads = pool, n_req, n_tokens, n_heads
+        n = pc_attn_workspace_bytes(pool.desc, n_req, n_tokens, n_heads)
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=pool.device)
+
+    def plan(self, seq, q_off, order=None, group_off=None, shared=None, n_groups=None, causal: bool = True,
+             stream=None):
+        """Request r is sequence seq[r] with the queries q_off[r] ..
+        q_off[r+1]-1, its last tokens; order .. n_groups: its groups, as
+        prefix_groups gives them, or none."""
+        pool, R = self.pool, self.n_req
+        _need(seq.numel() == R and q_off.numel() == R + 1, f"seq and q_off of {R} requests")
+        given = [x for x in (order, group_off, shared, n_groups) if x is not None]
+        _need(len(given) in (0, 4), "groups: all of order, group_off, shared and n_groups, or none")
+        if given:
+            _need([x.numel() for x in given] == [R, R + 1, R, 1], f"groups of {R} requests")
+        for x in given:
+            _list(x, pool.device, "groups")
+        with _on(pool.device, stream):
+            pc_attn_plan(pool.desc, _list(seq, pool.device, "seq"), _list(q_off, pool.device, "q_off"), self.n_tokens,
+                         self.n_heads, causal, order, group_off, shared, n_groups, self.workspace, pool.status, stream)
+
+    def attend(self, layer: int, q, out=None, lse=None, scale: Optional[float] = None, stream=None):
+        """softmax(scale q K^T) V for q [n_tokens, n_heads, dim], each query
+        over the tokens it sees; scale: 1 / sqrt(dim) unless given.  lse
+        (float32 [n_tokens, n_heads]): log of each row's sum of exponentials."""
+        pool = self.pool
+        with _on(pool.device, stream):
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            for x in (q, out):
+                pool._rows(x, self.n_heads, "q and out")
+                _need(x.shape[0] == self.n_tokens, f"q and out: {self.n_tokens} tokens")
+            _need(lse is None or (lse.shape == q.shape[:2] and lse.dtype == torch.float32 and lse.is_contiguous()
+                                  and lse.device == pool.device), "lse: a contiguous float32 [tokens, heads]")
+            if scale is None:
+                scale = 1.0 / math.sqrt(q.shape[2])
+            pc_attn(pool.desc, layer, make_rows(q), self.n_req, self.n_tokens, self.n_heads, scale, make_rows(out),
+                    lse, self.workspace, stream)
+        return out
