@@ -65,6 +65,13 @@ using as3 = __attribute__((address_space(3))) void;
 __device__ __forceinline__ void load_lds16(const void *g, void *l) {
     __builtin_amdgcn_global_load_lds((const as1 *)g, (as3 *)l, 16, 0, 0);
 }
+// The same without the compiler's knowledge that LDS is written, for buffers
+// that are waited for by hand: it would wait for all loads in flight before
+// the next read of any LDS.  There is no output register to be overwritten.
+__device__ __forceinline__ void load_lds16_later(const void *g, const void *l) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const as3 *)l);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(g) : "memory", "m0");
+}
 __device__ __forceinline__ s16x4 read_tr(const uint16_t *l) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)l);
 }
@@ -112,36 +119,61 @@ __device__ N plan_sum(N v, N *total, N *lds) {    // exclusive, over the workgro
     return before + x - v;
 }
 
-// One workgroup makes the list of items.  Segment i < n_req is the own tokens
-// of the request at place i of the order, segment n_req + g group g's shared
-// tokens.
+// A segment as the plan holds it: segment i < n_req is the own tokens of the
+// request at place i of the order, segment n_req + g group g's shared tokens.
+struct Segment {
+    int32_t t0, n_tok, kv0, kv1, seq, per, tiles, part;
+    int32_t first;      // its first item on the wide list, or -1 - that on the narrow one
+};
+
+// The last i of n with at[i] <= x, where at[0] <= x.
+__device__ __forceinline__ int last_at(const int32_t *at, int n, int x) {
+    int lo = 0;
+    for (int step = 1 << (31 - __clz(n)); step; step >>= 1)
+        if (lo + step < n && at[lo + step] <= x) lo += step;
+    return lo;
+}
+
+// One workgroup makes the list of items.  It is bound by latency: a request's
+// lengths are three dependent reads away, and what comes after is kept in
+// LDS, where each query and each item finds its request or segment by a
+// binary search.
 __global__ __launch_bounds__(kPlanThreads) void attn_plan(AttnPlanArgs a) {
     const pc_pages &p = a.p;
     const AttnWs &ws = a.ws;
-    const int R = a.n_req, S = 2 * R + 2, G = a.n_heads / p.n_kv_heads, Hk = p.n_kv_heads;
-    int32_t *t0 = ws.place, *n_tok = t0 + S, *kv0 = n_tok + S, *kv1 = kv0 + S, *seq = kv1 + S, *gof = seq + S,
-            *len_at = gof + S;
-    __shared__ int lds[kPlanThreads / 64];
+    const int R = a.n_req, G = a.n_heads / p.n_kv_heads, Hk = p.n_kv_heads;
+    extern __shared__ int32_t plan_lds[];
+    int32_t *t0 = plan_lds;             // [R + 1] first query, in the order
+    int32_t *goff = t0 + R + 1;         // [R + 1] group_off
+    int32_t *len = goff + R + 1;        // [R]
+    int32_t *seq = len + R;             // [R]
+    int32_t *group = seq + R;           // [R] or -1
+    int32_t *from = group + R;          // [R] first row of q, then the first token that is its own
+    int32_t *share = from + R;          // [R] blocks of the group, then tokens
+    __shared__ Segment seg[kPlanThreads];
+    __shared__ int32_t first_item[kPlanThreads];
     __shared__ int64_t lds64[kPlanThreads / 64];
     __shared__ int any_bad;
     __shared__ uint32_t seen[PC_MAX_BATCH / 32];
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool grouped = a.order != nullptr;
+    const int n_groups = grouped ? *a.n_groups : 0;
     if (tid < PC_MAX_BATCH / 32) seen[tid] = 0;
-    if (tid == 0) {
-        any_bad = *a.status != PC_OK;
-        *ws.head = AttnHead{0, 0, 0, 0};
-    }
-    if (tid < 32) reinterpret_cast<int32_t *>(reinterpret_cast<char *>(ws.head) + kZeroOffset)[tid] = 0;
+    if (tid == 0) any_bad = *a.status != PC_OK;
+    if (tid < 64) reinterpret_cast<int32_t *>(ws.head)[tid] = 0;
+    if (grouped)
+        for (int i = tid; i <= R; i += kPlanThreads) {
+            goff[i] = a.group_off[i];
+            if (i < R) share[i] = a.shared[i];
+        }
     __syncthreads();
     if (any_bad) return;
     // the requests at their places
-    const bool grouped = a.order != nullptr;
-    const int n_groups = grouped ? *a.n_groups : 0;
     bool bad = n_groups < 0 || n_groups > R;
     int64_t total = 0;
     for (int j0 = 0; j0 < R; j0 += kPlanThreads) {
         const int j = j0 + tid;
-        int n = 0, q0 = 0, s = 0, len = 0;
+        int n = 0, q0 = 0, s = 0, l = 0;
         if (j < R) {
             const uint32_t r = grouped ? (uint32_t)a.order[j] : (uint32_t)j;
             if (r >= (uint32_t)R || (atomicOr(&seen[r >> 5], 1u << (r & 31)) >> (r & 31) & 1)) {
@@ -151,90 +183,78 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan(AttnPlanArgs a) {
                 n = a.q_off[r + 1] - q0;
                 s = a.seq[r];
                 if (q0 < 0 || n < 0 || (int64_t)q0 + n > a.n_tokens || (uint32_t)s >= (uint32_t)p.n_seqs) bad = true;
-                else len = p.d_len[s];
-                if (len < 0 || (int64_t)len > (int64_t)p.table_width * kBlk) bad = true;
+                else l = p.d_len[s];
+                if (l < 0 || (int64_t)l > (int64_t)p.table_width * kBlk) bad = true;
             }
             if (bad) n = 0;
         }
         int64_t all;
-        const int at = (int)(total + plan_sum((int64_t)n, &all, lds64));
+        const int64_t at = total + plan_sum((int64_t)n, &all, lds64);
         if (j < R) {
-            t0[j] = at;
-            n_tok[j] = n;
+            t0[j] = (int32_t)at;
+            len[j] = l;
             seq[j] = s;
-            kv0[j] = 0;
-            kv1[j] = len;
-            gof[j] = q0;        // until the queries are listed
-            len_at[j] = len;
+            from[j] = q0;
+            group[j] = -1;
         }
         total += all;
     }
+    if (tid == 0) t0[R] = (int32_t)total;
     if (total != a.n_tokens) bad = true;    // every request once, so every query in one request
+    if (grouped)
+        for (int g = tid; g < n_groups && g < R; g += kPlanThreads)
+            bad |= goff[g] < 0 || goff[g + 1] < goff[g] || goff[g + 1] > R || (g == 0 && goff[0] != 0) ||
+                   (g == n_groups - 1 && goff[g + 1] != R);
     if (bad) any_bad = 1;
     __syncthreads();
     if (any_bad) {
         if (tid == 0) *a.status = PC_EINVAL;
         return;
     }
-    // queries in the order
-    const int lane = tid & 63, wave = tid >> 6;
-    for (int j = wave; j < R; j += kPlanThreads / 64) {
-        const int n = n_tok[j], q0 = gof[j], len = len_at[j], at = t0[j];
-        for (int i = lane; i < n; i += 64) {
-            ws.tok[at + i] = q0 + i;
-            ws.lim[at + i] = a.causal ? len - n + i + 1 : len;
-            ws.pos[at + i] = j;
-        }
+    // the queries in the order
+    for (int t = tid; t < (int)a.n_tokens; t += kPlanThreads) {
+        const int j = last_at(t0, R, t), i = t - t0[j], n = t0[j + 1] - t0[j];
+        ws.tok[t] = from[j] + i;
+        ws.lim[t] = a.causal ? len[j] - n + i + 1 : len[j];
+        ws.pos[t] = j;
     }
     __syncthreads();
-    for (int j = tid; j < R; j += kPlanThreads) gof[j] = -1;
+    for (int j = tid; j < R; j += kPlanThreads) from[j] = 0;
     __syncthreads();
-    // groups, a wave each: the tokens that all members share
+    // the tokens that all members of a group share: a wave for each group
     for (int g = wave; g < n_groups; g += kPlanThreads / 64) {
-        const int j0 = a.group_off[g], j1 = a.group_off[g + 1];
-        if (j0 < 0 || j1 < j0 || j1 > R || (g == 0 && j0 != 0) || (g == n_groups - 1 && j1 != R)) {
-            any_bad = 1;
-            continue;
-        }
-        int least = 0x7fffffff, rows = 0;
-        for (int j = j0 + lane; j < j1; j += 64) {
-            const int len = len_at[j];
-            least = len < least ? len : least;
-            rows += n_tok[j];
-        }
+        const int j0 = goff[g], j1 = goff[g + 1], blocks = share[g];
+        int least = 0x7fffffff;
+        for (int j = j0 + lane; j < j1; j += 64) least = min(least, len[j]);
 #pragma unroll
-        for (int d = 32; d; d >>= 1) {
-            const int y = __shfl_xor(least, d);
-            least = y < least ? y : least;
-            rows += __shfl_xor(rows, d);
-        }
-        const int blocks = a.shared[g];
+        for (int d = 32; d; d >>= 1) least = min(least, __shfl_xor(least, d));
         int tokens = j1 - j0 < 2 || blocks <= 0 ? 0 : least / kBlk * kBlk;
         if ((int64_t)blocks * kBlk < tokens) tokens = blocks * kBlk;
-        const int s = R + g;
-        if (lane == 0) {
-            t0[s] = j1 > j0 ? t0[j0] : 0;
-            n_tok[s] = tokens ? rows : 0;
-            kv0[s] = 0;
-            kv1[s] = tokens;
-            seq[s] = j1 > j0 ? seq[j0] : 0;
-        }
         if (tokens)
             for (int j = j0 + lane; j < j1; j += 64) {
-                kv0[j] = tokens;
-                gof[j] = g;
+                from[j] = tokens;
+                group[j] = g;
             }
+        if (lane == 0) share[g] = tokens;
     }
     __syncthreads();
-    if (any_bad) {
-        if (tid == 0) *a.status = PC_EINVAL;
-        return;
-    }
     // blocks of work on each list, and from them how long an item may be
     const int n_seg = R + n_groups;
+    auto segment = [&](int i) {     // groups before the requests' own tokens: theirs are the longest items
+        Segment x{};
+        if (i < n_groups) {
+            const int j0 = goff[i], j1 = goff[i + 1];
+            if (share[i]) x = Segment{t0[j0], t0[j1] - t0[j0], 0, share[i], seq[j0], 0, 0, 0, 0};
+        } else if (i < n_seg) {
+            const int j = i - n_groups;
+            x = Segment{t0[j], t0[j + 1] - t0[j], from[j], len[j], seq[j], 0, 0, 0, 0};
+        }
+        return x;
+    };
     int64_t wide = 0, narrow = 0;
-    for (int s = tid; s < n_seg; s += kPlanThreads) {
-        const int64_t rows = (int64_t)n_tok[s] * G, blocks = (kv1[s] - kv0[s] + kTileKv - 1) / kTileKv;
+    for (int i = tid; i < n_seg; i += kPlanThreads) {
+        const Segment x = segment(i);
+        const int64_t rows = (int64_t)x.n_tok * G, blocks = (x.kv1 - x.kv0 + kTileKv - 1) / kTileKv;
         if (rows > kNarrowRows) wide += (rows + kWideRows - 1) / kWideRows * blocks;
         else if (rows) narrow += blocks;
     }
@@ -246,59 +266,55 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan(AttnPlanArgs a) {
     const int len_wide = (int)(by_wide < kWideMinBlocks ? kWideMinBlocks : by_wide);
     const int len_narrow = (int)(by_narrow < kNarrowMinBlocks ? kNarrowMinBlocks : by_narrow);
     int n_wide = 0, n_narrow = 0, rows_at = 0;
-    // groups before the requests' own tokens: theirs are the longest items
     for (int i0 = 0; i0 < n_seg; i0 += kPlanThreads) {
-        const int i = i0 + tid, s = i < n_groups ? R + i : i - n_groups;
-        int chunks = 0, tiles = 0, per = 0, part = 0, st = 0, sn = 0, sb = 0, se = 0, ss = 0;
-        bool is_wide = false, direct = false;
-        if (i < n_seg) {
-            st = t0[s];
-            sn = n_tok[s];
-            sb = kv0[s];
-            se = kv1[s];
-            ss = seq[s];
-            const int64_t rows = (int64_t)sn * G;
-            const int blocks = (se - sb + kTileKv - 1) / kTileKv;
-            is_wide = rows > kNarrowRows;
-            if (rows && blocks) {
-                tiles = (int)((rows + kWideRows - 1) / kWideRows);
-                const int most = is_wide ? len_wide : len_narrow;
-                chunks = (blocks + most - 1) / most;
-                per = (blocks + chunks - 1) / chunks;
-                chunks = (blocks + per - 1) / per;
-                direct = s < R && chunks == 1 && gof[s] < 0;
-                part = direct ? 0 : chunks * sn * a.n_heads;
-            }
+        const int i = i0 + tid;
+        Segment x = segment(i);
+        int chunks = 0;
+        bool direct = false;
+        const int64_t rows = (int64_t)x.n_tok * G;
+        const int blocks = (x.kv1 - x.kv0 + kTileKv - 1) / kTileKv;
+        const bool is_wide = rows > kNarrowRows;
+        if (rows && blocks) {
+            x.tiles = (int)((rows + kWideRows - 1) / kWideRows);
+            const int most = is_wide ? len_wide : len_narrow;
+            chunks = (blocks + most - 1) / most;
+            const int per = (blocks + chunks - 1) / chunks;
+            chunks = (blocks + per - 1) / per;
+            x.per = per * kTileKv;
+            direct = i >= n_groups && chunks == 1 && group[i - n_groups] < 0;
         }
-        const int items = chunks * tiles * Hk;
-        int all_w, all_n, all_r;
-        const int at_w = n_wide + plan_sum(is_wide ? items : 0, &all_w, lds);
-        const int at_n = n_narrow + plan_sum(is_wide ? 0 : items, &all_n, lds);
-        const int at_r = rows_at + plan_sum(part, &all_r, lds);
-        n_wide += all_w;
-        n_narrow += all_n;
-        rows_at += all_r;
-        const int at = is_wide ? at_w : at_n;
+        const int items = chunks * x.tiles * Hk;
+        // items of this pass, wide and narrow ones, and partial rows, in one sum of two words
+        int64_t all_items, all_rest;
+        const int64_t at_items = plan_sum((int64_t)items << 32 | (is_wide ? items : 0), &all_items, lds64);
+        const int64_t at_rest = plan_sum((int64_t)(direct ? 0 : chunks * x.n_tok * a.n_heads), &all_rest, lds64);
+        const int before = (int)(at_items >> 32), wide_before = (int)(uint32_t)at_items;
+        x.first = is_wide ? n_wide + wide_before : -1 - (n_narrow + before - wide_before);
+        x.part = direct ? -1 : rows_at + (int)at_rest;
+        seg[tid] = x;
+        first_item[tid] = before;
         if (i < n_seg)      // own: at the request's place; groups': behind both lists, for now
-            ws.parts[s < R ? s : R + s] = direct ? AttnParts{-1, -1, 0, 0} : AttnParts{at_r, chunks, sn, st};
-        // the items of a wave's segments, one segment after the other
-        for (uint64_t left = __ballot(items > 0); left; left &= left - 1) {
-            const int k = __ffsll((unsigned long long)left) - 1;
-            const int xn = __shfl(items, k), xt = __shfl(tiles, k), xp = __shfl(per, k) * kTileKv, xa = __shfl(at, k);
-            const int x0 = __shfl(st, k), x1 = __shfl(sn, k), xb = __shfl(sb, k), xe = __shfl(se, k);
-            const int xs = __shfl(ss, k), xr = __shfl(at_r, k), xd = __shfl((int)direct, k);
-            AttnItem *to = (__shfl((int)is_wide, k) ? ws.wide : ws.narrow) + xa;
-            for (int x = lane; x < xn; x += 64) {
-                const int tile = x % xt, rest = x / xt, head = rest % Hk, c = rest / Hk;
-                const int b = xb + c * xp;
-                to[x] = AttnItem{x0, x1, b, b + xp < xe ? b + xp : xe, xs, head | tile << 8,
-                                 xd ? -1 : xr + c * x1 * a.n_heads, 0};
-            }
+            ws.parts[i < n_groups ? 2 * R + i : i - n_groups] =
+                direct ? AttnParts{-1, -1, 0, 0} : AttnParts{x.part, chunks, x.n_tok, x.t0};
+        __syncthreads();
+        const int n_items = (int)(all_items >> 32), n_here = min(n_seg - i0, kPlanThreads);
+        for (int u = tid; u < n_items; u += kPlanThreads) {
+            const int k = last_at(first_item, n_here, u);
+            const Segment y = seg[k];
+            const uint32_t off = u - first_item[k], rest = off / (uint32_t)y.tiles, tile = off - rest * y.tiles;
+            const uint32_t c = rest / (uint32_t)Hk, head = rest - c * Hk;
+            const int b = y.kv0 + (int)c * y.per;
+            AttnItem *to = y.first >= 0 ? ws.wide + y.first : ws.narrow + (-1 - y.first);
+            to[off] = AttnItem{y.t0, y.n_tok, b, min(b + y.per, y.kv1), y.seq, (int32_t)(head | tile << 8),
+                               y.part < 0 ? -1 : y.part + (int)c * y.n_tok * a.n_heads, 0};
         }
+        n_wide += (int)(uint32_t)all_items;
+        n_narrow += n_items - (int)(uint32_t)all_items;
+        rows_at += (int)all_rest;
+        __syncthreads();
     }
-    __syncthreads();
     for (int j = tid; j < R; j += kPlanThreads)
-        ws.parts[R + j] = gof[j] < 0 ? AttnParts{0, 0, 0, 0} : ws.parts[2 * R + gof[j]];
+        ws.parts[R + j] = group[j] < 0 ? AttnParts{0, 0, 0, 0} : ws.parts[2 * R + group[j]];
     if (tid == 0) *ws.head = AttnHead{1, n_wide, n_narrow, 0};
 }
 
@@ -353,21 +369,26 @@ __global__ __launch_bounds__(256, 2) void attn_wide(AttnArgs a) {
         const int tiles = end > it.kv0 ? (end - it.kv0 + kTileKv - 1) / kTileKv : 0;
         const int32_t *table = a.table + (int64_t)it.seq * a.table_width;
 
-        // a wave loads one page of each tile: 16 tokens
-        auto fetch = [&](int n, int buf) {
+        // a wave loads one page of each tile: 16 tokens.  The page's number is
+        // read a tile ahead, so that it is there when its loads are issued.
+        // (none: a zero that the compiler takes for a lane's own, or it would wait for the number
+        // at once to have it in a scalar register)
+        int none;
+        asm volatile("v_mov_b32 %0, 0" : "=v"(none));
+        auto page_of = [&](int n) { return table[min(it.kv0 + n * kTileKv + wave * kBlk, end - 1) / kBlk + none]; };
+        auto fetch = [&](int n, int buf, int number) {
+            const uint32_t page = min((uint32_t)__builtin_amdgcn_readfirstlane(number), (uint32_t)(a.n_pages - 1));
             const int t_first = it.kv0 + n * kTileKv + wave * kBlk;
-            const int page_at = min(t_first, end - 1) / kBlk;
-            const uint32_t page = min((uint32_t)table[page_at], (uint32_t)(a.n_pages - 1));
             const int64_t from = (int64_t)page * a.page_stride + (int64_t)head * a.head_stride;
-            uint16_t *lk = &lds_k[buf][wave * kBlk * D], *lv = &lds_v[buf][wave * kBlk * D];
+            const uint16_t *lk = &lds_k[buf][wave * kBlk * D], *lv = &lds_v[buf][wave * kBlk * D];
 #pragma unroll
             for (int i = 0; i < kPieces / 4; ++i) {
                 const int u = i * 64 + lane, t = u / kPieces, c = u % kPieces;
                 const int64_t at = from + t * a.token_stride;
-                load_lds16(kp + at + (c ^ (t & (kPieces - 1))) * 8, lk + i * 512);
+                load_lds16_later(kp + at + (c ^ (t & (kPieces - 1))) * 8, lk + i * 512);
                 // behind the end there may be anything, and zero times anything is to be zero
                 const uint16_t *v = vp + at + (c ^ (2 * t & (kPieces - 1))) * 8;
-                load_lds16(t_first + t < end ? v : zeros, lv + i * 512);
+                load_lds16_later(t_first + t < end ? v : zeros, lv + i * 512);
             }
         };
         f32x16 o[kDb];
@@ -376,11 +397,18 @@ __global__ __launch_bounds__(256, 2) void attn_wide(AttnArgs a) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[i][r] = 0;
         float m = kNegInf, l = 0;
-        if (tiles) fetch(0, 0);
+        int page = 0;
+        if (tiles) {
+            fetch(0, 0, page_of(0));
+            page = page_of(1);
+        }
         for (int n = 0; n < tiles; ++n) {
             wait_loads();
             __syncthreads();
-            if (n + 1 < tiles) fetch(n + 1, (n + 1) & 1);
+            if (n + 1 < tiles) {
+                fetch(n + 1, (n + 1) & 1, page);
+                page = page_of(n + 2);
+            }
             const uint16_t *lk = lds_k[n & 1], *lv = lds_v[n & 1];
             f32x16 s[2];
 #pragma unroll
@@ -621,26 +649,50 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a, int32_t n_req) {
         const int k = c < grp.chunks ? c : c - grp.chunks;
         return x.base + ((int64_t)k * x.n_tok + (t - x.t0)) * a.n_heads + h;
     };
-    float top = kNegInf;
-    for (int c = lane; c < n; c += 64) top = fmaxf(top, a.ws.lse[row(c)]);
+    // a lane holds one part's weight; the parts' values follow with all loads of four in flight
+    float top = kNegInf, sum = 0, o[2] = {0, 0};
+    for (int c0 = 0; c0 < n; c0 += 64) {
+        const int c = c0 + lane;
+        const int64_t r = c < n ? row(c) : 0;
+        const float lse = c < n ? a.ws.lse[r] : kNegInf;
+        float now = fmaxf(top, lse);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    float sum = 0, o[2] = {0, 0};
-    if (top != kNegInf)
-        for (int c = 0; c < n; ++c) {
-            const int64_t r = row(c);
-            const float lse = a.ws.lse[r];
-            if (lse == kNegInf) continue;
-            const float w = exp2_of(lse - top);
-            sum += w;
-            if (D == 128) {
-                const float2 x = *reinterpret_cast<const float2 *>(a.ws.o + r * D + 2 * lane);
-                o[0] += w * x.x;
-                o[1] += w * x.y;
-            } else {
-                o[0] += w * a.ws.o[r * D + lane];
+        for (int d = 32; d; d >>= 1) now = fmaxf(now, __shfl_xor(now, d));
+        if (now == kNegInf) continue;
+        const float f = exp2_of(top - now);
+        const float w = exp2_of(lse - now);
+        float all = w;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d);
+        sum = sum * f + all;
+        o[0] *= f;
+        o[1] *= f;
+        top = now;
+        const int m = min(n - c0, 64);
+        for (int k0 = 0; k0 < m; k0 += 8) {
+            float x[8][2], wk[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                // the values of an empty part are not written: its weight is 0
+                const int from = min(k0 + k, m - 1);
+                wk[k] = k0 + k < m ? __shfl(w, from) : 0.f;
+                const int64_t rk = ((int64_t)__shfl((int)(r >> 32), from) << 32) | (uint32_t)__shfl((int)r, from);
+                if (D == 128) {
+                    const float2 v = *reinterpret_cast<const float2 *>(a.ws.o + rk * D + 2 * lane);
+                    x[k][0] = v.x;
+                    x[k][1] = v.y;
+                } else {
+                    x[k][0] = a.ws.o[rk * D + lane];
+                    x[k][1] = 0;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                o[0] += wk[k] == 0.f ? 0.f : wk[k] * x[k][0];
+                o[1] += wk[k] == 0.f ? 0.f : wk[k] * x[k][1];
             }
         }
+    }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int64_t q_row = a.ws.tok[t];
     uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + h * a.out_head;
@@ -675,7 +727,7 @@ int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_h
     int64_t o = 0;
     auto take = [&](int64_t bytes) { const int64_t at = o; o += up(bytes); return at; };
     const int64_t head = take(256), tok = take(4 * n_tokens), lim = take(4 * n_tokens), pos = take(4 * n_tokens),
-                  place = take(7 * 4 * (2LL * n_req + 2)), parts = take(3LL * n_req * (int64_t)sizeof(AttnParts)),
+                  parts = take(3LL * n_req * (int64_t)sizeof(AttnParts)),
                   w = take(wide * (int64_t)sizeof(AttnItem)), nr = take(narrow * (int64_t)sizeof(AttnItem)),
                   po = take(rows * head_dim * 4), pl = take(rows * 4);
     if (ws) {
@@ -683,7 +735,6 @@ int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_h
         ws->tok = reinterpret_cast<int32_t *>(base + tok);
         ws->lim = reinterpret_cast<int32_t *>(base + lim);
         ws->pos = reinterpret_cast<int32_t *>(base + pos);
-        ws->place = reinterpret_cast<int32_t *>(base + place);
         ws->parts = reinterpret_cast<AttnParts *>(base + parts);
         ws->wide = reinterpret_cast<AttnItem *>(base + w);
         ws->narrow = reinterpret_cast<AttnItem *>(base + nr);
@@ -695,7 +746,13 @@ int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_h
 }
 
 hipError_t launch_attn_plan(const AttnPlanArgs &a, hipStream_t st) {
-    attn_plan<<<1, kPlanThreads, 0, st>>>(a);
+    const size_t bytes = 4 * (7 * (size_t)a.n_req + 2);
+    if (bytes > 16 * 1024) {    // beside the kernel's own 48 KiB
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_plan),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e != hipSuccess) return e;
+    }
+    attn_plan<<<1, kPlanThreads, bytes, st>>>(a);
     return hipGetLastError();
 }
 

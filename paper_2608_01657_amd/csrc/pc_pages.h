@@ -74,7 +74,6 @@ struct AttnWs {
     int32_t *tok;           // [n_tokens] query row of the query at this place of the order
     int32_t *lim;           // [n_tokens] it sees the tokens before this one
     int32_t *pos;           // [n_tokens] its request's place in the order
-    int32_t *place;         // [7][2 n_req + 2] the plan's own
     AttnParts *parts;       // [3][n_req]: own, group, and groups by number
     AttnItem *wide, *narrow;
     float *o;               // [rows][head_dim] partial results, normalised
