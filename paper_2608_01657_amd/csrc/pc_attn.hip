@@ -84,14 +84,16 @@ __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf
 // Every load of the wave has landed in LDS.
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// The item of a workgroup's (or wave's) turn: workgroups go round the eight
-// XCDs, and neighbouring items (row tiles of the same tokens) share an L2
-// where they are on one.
+// The item of a workgroup's turn.  Workgroups go round the eight XCDs, each
+// with an L2 of its own: runs of kRun neighbouring items (row tiles of the
+// same tokens) go to one XCD, and the runs round the XCDs, so that the long
+// items at the front of the list are spread over all.
+constexpr int kRun = 8;
 __device__ __forceinline__ int xcd_item(int turn, int n) {
-    const int per = (n + 7) / 8, at = (turn & 7) * per + (turn >> 3);
-    return turn >> 3 < per && at < n ? at : -1;
+    const int k = turn >> 3, at = (k / kRun * 8 + (turn & 7)) * kRun + k % kRun;
+    return at < n ? at : -1;
 }
-__device__ __forceinline__ int xcd_turns(int n) { return (n + 7) / 8 * 8; }
+__device__ __forceinline__ int xcd_turns(int n) { return (n + 8 * kRun - 1) / (8 * kRun) * (8 * kRun); }
 
 // ------------------------------------------------------------------ plan
 
