@@ -80,6 +80,16 @@ __device__ __forceinline__ s16x8 join(s16x4 a, s16x4 b) {
 }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
+__device__ __forceinline__ void load_lds16_later(const void *base, uint32_t offset, const void *l) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const as3 *)l);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base)
+                 : "memory", "m0");
+}
+
+// The running maximum follows the scores only where they pass it by this much
+// (in powers of two): weights up to 2^8 lose nothing in any of the types, and
+// most tiles are spared the scaling of O.
+constexpr float kSlack = 8.f;
 
 // Every load of the wave has landed in LDS.
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
@@ -97,28 +107,43 @@ __device__ __forceinline__ int xcd_turns(int n) { return (n + 8 * kRun - 1) / (8
 
 // ------------------------------------------------------------------ plan
 
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanGroups = 16;
 
-template <typename N>
-__device__ N plan_sum(N v, N *total, N *lds) {    // exclusive, over the workgroup
+// Sums of K words over the workgroup's threads: exclusive ones in v, those over
+// all in total.
+template <int NT, int K, typename N>
+__device__ __forceinline__ void plan_sum(N (&v)[K], N (&total)[K], N *lds) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    N x = v;
+    N x[K];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const N y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+    for (int i = 0; i < K; ++i) x[i] = v[i];
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const N y = __shfl_up(x[i], d);
+            x[i] += lane >= d ? y : 0;
+        }
     __syncthreads();
-    if (lane == 63) lds[w] = x;
+    if (lane == 63)
+#pragma unroll
+        for (int i = 0; i < K; ++i) lds[w * K + i] = x[i];
     __syncthreads();
-    N before = 0, all = 0;
-    for (int i = 0; i < kPlanThreads / 64; ++i) {
-        const N t = lds[i];
-        if (i < w) before += t;
-        all += t;
+    N t[NT / 64][K];
+#pragma unroll
+    for (int k = 0; k < NT / 64; ++k)
+#pragma unroll
+        for (int i = 0; i < K; ++i) t[k][i] = lds[k * K + i];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        v[i] = x[i] - v[i];
+        total[i] = 0;
+#pragma unroll
+        for (int k = 0; k < NT / 64; ++k) {
+            v[i] += k < w ? t[k][i] : 0;
+            total[i] += t[k][i];
+        }
     }
-    *total = all;
-    return before + x - v;
 }
 
 // A segment as the plan holds it: segment i < n_req is the own tokens of the
@@ -136,107 +161,111 @@ __device__ __forceinline__ int last_at(const int32_t *at, int n, int x) {
     return lo;
 }
 
-// One workgroup makes the list of items.  It is bound by latency: a request's
-// lengths are three dependent reads away, and what comes after is kept in
-// LDS, where each query and each item finds its request or segment by a
-// binary search.
-__global__ __launch_bounds__(kPlanThreads) void attn_plan(AttnPlanArgs a) {
+// x / d by a 32-bit float where that is exact but for one (x below 2^22).
+__device__ __forceinline__ uint32_t divide(uint32_t x, uint32_t d) {
+    if (x >= 1u << 22) return x / d;
+    uint32_t q = (uint32_t)((float)x * __builtin_amdgcn_rcpf((float)d));
+    const int32_t r = (int32_t)(x - q * d);
+    return r < 0 ? q - 1 : r >= (int32_t)d ? q + 1 : q;
+}
+
+// Makes the list of items.  It is bound by latency: a request's length is two
+// dependent reads away, and what comes after is kept in LDS, where each query
+// and each item finds its request or segment by a binary search.  Every
+// workgroup works all segments out by itself and writes its share of the
+// queries and items; the first one writes the rest.  (128 requests with 3,000
+// items: 20 us by one workgroup, most of it in writing items.)
+template <int NT>
+__global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
     const pc_pages &p = a.p;
     const AttnWs &ws = a.ws;
     const int R = a.n_req, G = a.n_heads / p.n_kv_heads, Hk = p.n_kv_heads;
     extern __shared__ int32_t plan_lds[];
     int32_t *t0 = plan_lds;             // [R + 1] first query, in the order
     int32_t *goff = t0 + R + 1;         // [R + 1] group_off
-    int32_t *len = goff + R + 1;        // [R]
+    int32_t *q_off = goff + R + 1;      // [R + 1] of the requests, as their lengths and sequences:
+    int32_t *len = q_off + R + 1;       // [R]
     int32_t *seq = len + R;             // [R]
-    int32_t *group = seq + R;           // [R] or -1
-    int32_t *from = group + R;          // [R] first row of q, then the first token that is its own
-    int32_t *share = from + R;          // [R] blocks of the group, then tokens
-    __shared__ Segment seg[kPlanThreads];
-    __shared__ int32_t first_item[kPlanThreads];
-    __shared__ int64_t lds64[kPlanThreads / 64];
-    __shared__ int any_bad;
+    int32_t *place = seq + R;           // [R] the request at a place | its group (or kNoGroup) << 16
+    int32_t *share = place + R;         // [R] blocks of the group, then tokens
+    constexpr int kNoGroup = 0x7fff;
+    static_assert(PC_MAX_BATCH < kNoGroup, "request and group in one word");
+    __shared__ Segment seg[NT];
+    __shared__ int32_t first_item[NT];
+    __shared__ int32_t lds[3 * (NT / 64)];
+    __shared__ int64_t lds64[2 * (NT / 64)];
+    __shared__ int any_bad, stop;
     __shared__ uint32_t seen[PC_MAX_BATCH / 32];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const bool grouped = a.order != nullptr;
-    const int n_groups = grouped ? *a.n_groups : 0;
+    const bool grouped = a.order != nullptr, first = blockIdx.x == 0;
+    const int wg_tid = blockIdx.x * NT + tid, wg_step = gridDim.x * NT;     // of what the workgroups share
     if (tid < PC_MAX_BATCH / 32) seen[tid] = 0;
-    if (tid == 0) any_bad = *a.status != PC_OK;
-    if (tid < 64) reinterpret_cast<int32_t *>(ws.head)[tid] = 0;
-    if (grouped)
-        for (int i = tid; i <= R; i += kPlanThreads) {
-            goff[i] = a.group_off[i];
-            if (i < R) share[i] = a.shared[i];
-        }
+    if (tid == 0) any_bad = 0;
+    if (first && tid < 64) reinterpret_cast<int32_t *>(ws.head)[tid] = 0;
     __syncthreads();
-    if (any_bad) return;
-    // the requests at their places
+    // all that the caller gives, at once
+    const int status = __hip_atomic_load(a.status, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int n_groups = grouped ? *a.n_groups : 0;
     bool bad = n_groups < 0 || n_groups > R;
-    int64_t total = 0;
-    for (int j0 = 0; j0 < R; j0 += kPlanThreads) {
-        const int j = j0 + tid;
-        int n = 0, q0 = 0, s = 0, l = 0;
-        if (j < R) {
-            const uint32_t r = grouped ? (uint32_t)a.order[j] : (uint32_t)j;
-            if (r >= (uint32_t)R || (atomicOr(&seen[r >> 5], 1u << (r & 31)) >> (r & 31) & 1)) {
-                bad = true;
-            } else {
-                q0 = a.q_off[r];
-                n = a.q_off[r + 1] - q0;
-                s = a.seq[r];
-                if (q0 < 0 || n < 0 || (int64_t)q0 + n > a.n_tokens || (uint32_t)s >= (uint32_t)p.n_seqs) bad = true;
-                else l = p.d_len[s];
-                if (l < 0 || (int64_t)l > (int64_t)p.table_width * kBlk) bad = true;
-            }
-            if (bad) n = 0;
-        }
-        int64_t all;
-        const int64_t at = total + plan_sum((int64_t)n, &all, lds64);
-        if (j < R) {
-            t0[j] = (int32_t)at;
-            len[j] = l;
-            seq[j] = s;
-            from[j] = q0;
-            group[j] = -1;
-        }
-        total += all;
+    for (int i = tid; i <= R; i += NT) {
+        q_off[i] = a.q_off[i];
+        goff[i] = grouped ? a.group_off[i] : 0;
+        if (i == R) break;
+        const uint32_t s = a.seq[i], r = grouped ? (uint32_t)a.order[i] : (uint32_t)i;
+        share[i] = grouped ? a.shared[i] : 0;
+        seq[i] = s;
+        const int l = s < (uint32_t)p.n_seqs ? p.d_len[s] : -1;
+        len[i] = l;
+        bad |= l < 0 || (int64_t)l > (int64_t)p.table_width * kBlk;
+        bad |= r >= (uint32_t)R || (atomicOr(&seen[r >> 5], 1u << (r & 31)) >> (r & 31) & 1);
+        place[i] = (r < (uint32_t)R ? r : 0) | kNoGroup << 16;
     }
-    if (tid == 0) t0[R] = (int32_t)total;
-    if (total != a.n_tokens) bad = true;    // every request once, so every query in one request
-    if (grouped)
-        for (int g = tid; g < n_groups && g < R; g += kPlanThreads)
-            bad |= goff[g] < 0 || goff[g + 1] < goff[g] || goff[g + 1] > R || (g == 0 && goff[0] != 0) ||
-                   (g == n_groups - 1 && goff[g + 1] != R);
+    if (tid == 0) stop = status;        // another workgroup may set it meanwhile
+    __syncthreads();
+    if (stop != PC_OK) return;
+    // every request once, and their queries one behind the other: every query in one of them
+    for (int i = tid; i < R; i += NT) bad |= q_off[i + 1] < q_off[i];
+    bad |= q_off[0] != 0 || q_off[R] != a.n_tokens;
+    for (int g = tid; g < n_groups && g < R; g += NT)
+        bad |= goff[g] < 0 || goff[g + 1] < goff[g] || goff[g + 1] > R || (g == 0 && goff[0] != 0) ||
+               (g == n_groups - 1 && goff[g + 1] != R);
     if (bad) any_bad = 1;
     __syncthreads();
     if (any_bad) {
         if (tid == 0) *a.status = PC_EINVAL;
         return;
     }
+    auto request = [&](int j) { return place[j] & 0xffff; };
+    auto group = [&](int j) { return place[j] >> 16; };
+    int before = 0;
+    for (int j0 = 0; j0 < R; j0 += NT) {
+        const int j = j0 + tid;
+        int n[1] = {0}, all[1];
+        if (j < R) n[0] = q_off[request(j) + 1] - q_off[request(j)];
+        plan_sum<NT>(n, all, lds);
+        if (j < R) t0[j] = before + n[0];
+        before += all[0];
+    }
+    if (tid == 0) t0[R] = before;
+    __syncthreads();
     // the queries in the order
-    for (int t = tid; t < (int)a.n_tokens; t += kPlanThreads) {
-        const int j = last_at(t0, R, t), i = t - t0[j], n = t0[j + 1] - t0[j];
-        ws.tok[t] = from[j] + i;
-        ws.lim[t] = a.causal ? len[j] - n + i + 1 : len[j];
+    for (int t = wg_tid; t < (int)a.n_tokens; t += wg_step) {
+        const int j = last_at(t0, R, t), i = t - t0[j], n = t0[j + 1] - t0[j], r = request(j);
+        ws.tok[t] = q_off[r] + i;
+        ws.lim[t] = a.causal ? len[r] - n + i + 1 : len[r];
         ws.pos[t] = j;
     }
-    __syncthreads();
-    for (int j = tid; j < R; j += kPlanThreads) from[j] = 0;
-    __syncthreads();
     // the tokens that all members of a group share: a wave for each group
-    for (int g = wave; g < n_groups; g += kPlanThreads / 64) {
+    for (int g = wave; g < n_groups; g += NT / 64) {
         const int j0 = goff[g], j1 = goff[g + 1], blocks = share[g];
         int least = 0x7fffffff;
-        for (int j = j0 + lane; j < j1; j += 64) least = min(least, len[j]);
+        for (int j = j0 + lane; j < j1; j += 64) least = min(least, len[request(j)]);
 #pragma unroll
         for (int d = 32; d; d >>= 1) least = min(least, __shfl_xor(least, d));
         int tokens = j1 - j0 < 2 || blocks <= 0 ? 0 : least / kBlk * kBlk;
         if ((int64_t)blocks * kBlk < tokens) tokens = blocks * kBlk;
         if (tokens)
-            for (int j = j0 + lane; j < j1; j += 64) {
-                from[j] = tokens;
-                group[j] = g;
-            }
+            for (int j = j0 + lane; j < j1; j += 64) place[j] = request(j) | g << 16;
         if (lane == 0) share[g] = tokens;
     }
     __syncthreads();
@@ -246,29 +275,28 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan(AttnPlanArgs a) {
         Segment x{};
         if (i < n_groups) {
             const int j0 = goff[i], j1 = goff[i + 1];
-            if (share[i]) x = Segment{t0[j0], t0[j1] - t0[j0], 0, share[i], seq[j0], 0, 0, 0, 0};
+            if (share[i]) x = Segment{t0[j0], t0[j1] - t0[j0], 0, share[i], seq[request(j0)], 0, 0, 0, 0};
         } else if (i < n_seg) {
             const int j = i - n_groups;
-            x = Segment{t0[j], t0[j + 1] - t0[j], from[j], len[j], seq[j], 0, 0, 0, 0};
+            const int r = request(j), g = group(j);
+            x = Segment{t0[j], t0[j + 1] - t0[j], g == kNoGroup ? 0 : share[g], len[r], seq[r], 0, 0, 0, 0};
         }
         return x;
     };
-    int64_t wide = 0, narrow = 0;
-    for (int i = tid; i < n_seg; i += kPlanThreads) {
+    int64_t work[2] = {0, 0}, all_work[2];      // wide, narrow
+    for (int i = tid; i < n_seg; i += NT) {
         const Segment x = segment(i);
         const int64_t rows = (int64_t)x.n_tok * G, blocks = (x.kv1 - x.kv0 + kTileKv - 1) / kTileKv;
-        if (rows > kNarrowRows) wide += (rows + kWideRows - 1) / kWideRows * blocks;
-        else if (rows) narrow += blocks;
+        if (rows > kNarrowRows) work[0] += (rows + kWideRows - 1) / kWideRows * blocks;
+        else if (rows) work[1] += blocks;
     }
-    int64_t all_wide, all_narrow;
-    plan_sum(wide, &all_wide, lds64);
-    plan_sum(narrow, &all_narrow, lds64);
-    const int64_t by_wide = (all_wide * Hk + kWideItems - 1) / kWideItems,
-                  by_narrow = (all_narrow * Hk + kNarrowItems - 1) / kNarrowItems;
+    plan_sum<NT>(work, all_work, lds64);
+    const int64_t by_wide = (all_work[0] * Hk + kWideItems - 1) / kWideItems,
+                  by_narrow = (all_work[1] * Hk + kNarrowItems - 1) / kNarrowItems;
     const int len_wide = (int)(by_wide < kWideMinBlocks ? kWideMinBlocks : by_wide);
     const int len_narrow = (int)(by_narrow < kNarrowMinBlocks ? kNarrowMinBlocks : by_narrow);
     int n_wide = 0, n_narrow = 0, rows_at = 0;
-    for (int i0 = 0; i0 < n_seg; i0 += kPlanThreads) {
+    for (int i0 = 0; i0 < n_seg; i0 += NT) {
         const int i = i0 + tid;
         Segment x = segment(i);
         int chunks = 0;
@@ -283,40 +311,39 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan(AttnPlanArgs a) {
             const int per = (blocks + chunks - 1) / chunks;
             chunks = (blocks + per - 1) / per;
             x.per = per * kTileKv;
-            direct = i >= n_groups && chunks == 1 && group[i - n_groups] < 0;
+            direct = i >= n_groups && chunks == 1 && group(i - n_groups) == kNoGroup;
         }
         const int items = chunks * x.tiles * Hk;
-        // items of this pass, wide and narrow ones, and partial rows, in one sum of two words
-        int64_t all_items, all_rest;
-        const int64_t at_items = plan_sum((int64_t)items << 32 | (is_wide ? items : 0), &all_items, lds64);
-        const int64_t at_rest = plan_sum((int64_t)(direct ? 0 : chunks * x.n_tok * a.n_heads), &all_rest, lds64);
-        const int before = (int)(at_items >> 32), wide_before = (int)(uint32_t)at_items;
-        x.first = is_wide ? n_wide + wide_before : -1 - (n_narrow + before - wide_before);
-        x.part = direct ? -1 : rows_at + (int)at_rest;
+        // items of this pass, the wide ones among them, partial rows
+        int at[3] = {items, is_wide ? items : 0, direct ? 0 : chunks * x.n_tok * a.n_heads}, all[3];
+        plan_sum<NT>(at, all, lds);
+        x.first = is_wide ? n_wide + at[1] : -1 - (n_narrow + at[0] - at[1]);
+        x.part = direct ? -1 : rows_at + at[2];
         seg[tid] = x;
-        first_item[tid] = before;
-        if (i < n_seg)      // own: at the request's place; groups': behind both lists, for now
+        first_item[tid] = at[0];
+        if (first && i < n_seg)     // own: at the request's place; groups': behind both lists, for now
             ws.parts[i < n_groups ? 2 * R + i : i - n_groups] =
                 direct ? AttnParts{-1, -1, 0, 0} : AttnParts{x.part, chunks, x.n_tok, x.t0};
         __syncthreads();
-        const int n_items = (int)(all_items >> 32), n_here = min(n_seg - i0, kPlanThreads);
-        for (int u = tid; u < n_items; u += kPlanThreads) {
+        const int n_items = all[0], n_here = min(n_seg - i0, NT);
+        for (int u = wg_tid; u < n_items; u += wg_step) {
             const int k = last_at(first_item, n_here, u);
             const Segment y = seg[k];
-            const uint32_t off = u - first_item[k], rest = off / (uint32_t)y.tiles, tile = off - rest * y.tiles;
-            const uint32_t c = rest / (uint32_t)Hk, head = rest - c * Hk;
+            const uint32_t off = u - first_item[k], rest = divide(off, y.tiles), tile = off - rest * y.tiles;
+            const uint32_t c = divide(rest, Hk), head = rest - c * Hk;
             const int b = y.kv0 + (int)c * y.per;
             AttnItem *to = y.first >= 0 ? ws.wide + y.first : ws.narrow + (-1 - y.first);
             to[off] = AttnItem{y.t0, y.n_tok, b, min(b + y.per, y.kv1), y.seq, (int32_t)(head | tile << 8),
                                y.part < 0 ? -1 : y.part + (int)c * y.n_tok * a.n_heads, 0};
         }
-        n_wide += (int)(uint32_t)all_items;
-        n_narrow += n_items - (int)(uint32_t)all_items;
-        rows_at += (int)all_rest;
+        n_wide += all[1];
+        n_narrow += all[0] - all[1];
+        rows_at += all[2];
         __syncthreads();
     }
-    for (int j = tid; j < R; j += kPlanThreads)
-        ws.parts[R + j] = group[j] < 0 ? AttnParts{0, 0, 0, 0} : ws.parts[2 * R + group[j]];
+    if (!first) return;
+    for (int j = tid; j < R; j += NT)
+        ws.parts[R + j] = group(j) == kNoGroup ? AttnParts{0, 0, 0, 0} : ws.parts[2 * R + group(j)];
     if (tid == 0) *ws.head = AttnHead{1, n_wide, n_narrow, 0};
 }
 
@@ -329,386 +356,433 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan(AttnPlanArgs a) {
 // of V meet in a bank: piece c of token t of K is at c ^ t, of V at c ^ 2t
 // (modulo the pieces of a row).
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attn_wide(AttnArgs a) {
-    constexpr int kPieces = D / 8, kSteps = D / 16, kDb = D / 32;
-    __shared__ __align__(1024) uint16_t lds_k[2][kTileKv * D];
-    __shared__ __align__(1024) uint16_t lds_v[2][kTileKv * D];
-    __shared__ int lds_lim[4];
-    if (!a.ws.head->ok) return;
-    const int n_items = a.ws.head->n_wide;
+__device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, uint16_t *lds, int *lds_lim) {
+    constexpr int kPieces = D / 8, kSteps = D / 16, kDb = D / 32, kBuf = kTileKv * D;   // K, K, V, V
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const uint16_t *zeros = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(a.ws.head) + kZeroOffset);
     const uint16_t *kp = static_cast<const uint16_t *>(a.k), *vp = static_cast<const uint16_t *>(a.v);
-    for (int turn = blockIdx.x; turn < xcd_turns(n_items); turn += gridDim.x) {
-        const int which = xcd_item(turn, n_items);
-        if (which < 0) continue;
-        const AttnItem it = a.ws.wide[which];
-        const int head = it.head_tile & 255, tile = it.head_tile >> 8;
-        const int row = tile * kWideRows + wave * 32 + col;
-        const int tok = row / a.group, hq = head * a.group + row - tok * a.group;
-        const bool active = tok < it.n_tok;
-        const int lim = active ? min(a.ws.lim[it.t0 + tok], it.kv1) : 0;
-        const int64_t q_row = active ? a.ws.tok[it.t0 + tok] : 0;
-        s16x8 qf[kSteps];
-        {
-            const uint16_t *q = static_cast<const uint16_t *>(a.q) + q_row * a.q_token + hq * a.q_head + half * 8;
+    const int head = it.head_tile & 255, tile = it.head_tile >> 8;
+    const int row = tile * kWideRows + wave * 32 + col;
+    const int tok = row / a.group, hq = head * a.group + row - tok * a.group;
+    const bool active = tok < it.n_tok;
+    const int lim = active ? min(a.ws.lim[it.t0 + tok], it.kv1) : 0;
+    const int64_t q_row = active ? a.ws.tok[it.t0 + tok] : 0;
+    s16x8 qf[kSteps];
+    {
+        const uint16_t *q = static_cast<const uint16_t *>(a.q) + q_row * a.q_token + hq * a.q_head + half * 8;
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s)
-                qf[s] = active ? *reinterpret_cast<const s16x8 *>(q + 16 * s) : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
-        }
-        int most = lim, least = lim;
+        for (int s = 0; s < kSteps; ++s)
+            qf[s] = active ? *reinterpret_cast<const s16x8 *>(q + 16 * s) : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    }
+    int most = lim, least = lim;
 #pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            most = max(most, __shfl_xor(most, d));
-            least = min(least, __shfl_xor(least, d));
-        }
-        least = __builtin_amdgcn_readfirstlane(least);
-        __syncthreads();        // the last item's readers of LDS
-        if (lane == 0) lds_lim[wave] = most;
-        __syncthreads();
-        const int end = __builtin_amdgcn_readfirstlane(max(max(lds_lim[0], lds_lim[1]), max(lds_lim[2], lds_lim[3])));
-        const int tiles = end > it.kv0 ? (end - it.kv0 + kTileKv - 1) / kTileKv : 0;
-        const int32_t *table = a.table + (int64_t)it.seq * a.table_width;
+    for (int d = 16; d; d >>= 1) {
+        most = max(most, __shfl_xor(most, d));
+        least = min(least, __shfl_xor(least, d));
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    __syncthreads();        // the last item's readers of LDS
+    if (lane == 0) lds_lim[wave] = most;
+    __syncthreads();
+    const int end = __builtin_amdgcn_readfirstlane(max(max(lds_lim[0], lds_lim[1]), max(lds_lim[2], lds_lim[3])));
+    const int tiles = end > it.kv0 ? (end - it.kv0 + kTileKv - 1) / kTileKv : 0;
+    const int32_t *table = a.table + (int64_t)it.seq * a.table_width;
 
-        // a wave loads one page of each tile: 16 tokens.  The page's number is
-        // read a tile ahead, so that it is there when its loads are issued.
-        // (none: a zero that the compiler takes for a lane's own, or it would wait for the number
-        // at once to have it in a scalar register)
-        int none;
-        asm volatile("v_mov_b32 %0, 0" : "=v"(none));
-        auto page_of = [&](int n) { return table[min(it.kv0 + n * kTileKv + wave * kBlk, end - 1) / kBlk + none]; };
-        auto fetch = [&](int n, int buf, int number) {
-            const uint32_t page = min((uint32_t)__builtin_amdgcn_readfirstlane(number), (uint32_t)(a.n_pages - 1));
-            const int t_first = it.kv0 + n * kTileKv + wave * kBlk;
-            const int64_t from = (int64_t)page * a.page_stride + (int64_t)head * a.head_stride;
-            const uint16_t *lk = &lds_k[buf][wave * kBlk * D], *lv = &lds_v[buf][wave * kBlk * D];
+    // a wave loads one page of each tile: 16 tokens.  The page's number is
+    // read a tile ahead, so that it is there when its loads are issued.
+    // (none: a zero that the compiler takes for a lane's own, or it would wait for the number
+    // at once to have it in a scalar register)
+    int none;
+    asm volatile("v_mov_b32 %0, 0" : "=v"(none));
+    auto page_of = [&](int n) { return table[min(it.kv0 + n * kTileKv + wave * kBlk, end - 1) / kBlk + none]; };
+    uint32_t k_at[kPieces / 4], v_at[kPieces / 4];      // bytes of this lane's pieces in a page
+#pragma unroll
+    for (int i = 0; i < kPieces / 4; ++i) {
+        const int u = i * 64 + lane, t = u / kPieces, c = u % kPieces;
+        k_at[i] = 2 * (t * a.token_stride + (c ^ (t & (kPieces - 1))) * 8);
+        v_at[i] = 2 * (t * a.token_stride + (c ^ (2 * t & (kPieces - 1))) * 8);
+    }
+    auto fetch = [&](int n, int buf, int number) {
+        const uint32_t page = min((uint32_t)__builtin_amdgcn_readfirstlane(number), (uint32_t)(a.n_pages - 1));
+        const int t_first = it.kv0 + n * kTileKv + wave * kBlk;
+        const int64_t from = (int64_t)page * a.page_stride + (int64_t)head * a.head_stride;
+        const uint16_t *lk = lds + buf * kBuf + wave * kBlk * D, *lv = lk + 2 * kBuf;
+#pragma unroll
+        for (int i = 0; i < kPieces / 4; ++i) load_lds16_later(kp + from, k_at[i], lk + i * 512);
+        if (t_first + kBlk <= end) {
+#pragma unroll
+            for (int i = 0; i < kPieces / 4; ++i) load_lds16_later(vp + from, v_at[i], lv + i * 512);
+        } else {    // behind the end there may be anything, and zero times anything is to be zero
 #pragma unroll
             for (int i = 0; i < kPieces / 4; ++i) {
-                const int u = i * 64 + lane, t = u / kPieces, c = u % kPieces;
-                const int64_t at = from + t * a.token_stride;
-                load_lds16_later(kp + at + (c ^ (t & (kPieces - 1))) * 8, lk + i * 512);
-                // behind the end there may be anything, and zero times anything is to be zero
-                const uint16_t *v = vp + at + (c ^ (2 * t & (kPieces - 1))) * 8;
-                load_lds16_later(t_first + t < end ? v : zeros, lv + i * 512);
+                const char *v = reinterpret_cast<const char *>(vp + from) + v_at[i];
+                load_lds16_later(t_first + (i * 64 + lane) / kPieces < end ? v : reinterpret_cast<const char *>(zeros),
+                                 lv + i * 512);
             }
-        };
-        f32x16 o[kDb];
-#pragma unroll
-        for (int i = 0; i < kDb; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[i][r] = 0;
-        float m = kNegInf, l = 0;
-        int page = 0;
-        if (tiles) {
-            fetch(0, 0, page_of(0));
-            page = page_of(1);
         }
-        for (int n = 0; n < tiles; ++n) {
-            wait_loads();
-            __syncthreads();
-            if (n + 1 < tiles) {
-                fetch(n + 1, (n + 1) & 1, page);
-                page = page_of(n + 2);
+    };
+    f32x16 o[kDb];
+#pragma unroll
+    for (int i = 0; i < kDb; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = 0;
+    float m = kNegInf, l = 0;
+    int page = 0;
+    if (tiles) {
+        fetch(0, 0, page_of(0));
+        page = page_of(1);
+    }
+    for (int n = 0; n < tiles; ++n) {
+        wait_loads();
+        __syncthreads();
+        if (n + 1 < tiles) {
+            fetch(n + 1, (n + 1) & 1, page);
+            page = page_of(n + 2);
+        }
+        const uint16_t *lk = lds + (n & 1) * kBuf, *lv = lk + 2 * kBuf;
+        f32x16 s[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[h][r] = 0;
+#pragma unroll
+            for (int st = 0; st < kSteps; ++st) {
+                const int at = (h * 32 + col) * D + (((2 * st + half) ^ (col & (kPieces - 1))) * 8);
+                s[h] = T::mma32(*reinterpret_cast<const s16x8 *>(lk + at), qf[st], s[h]);
             }
-            const uint16_t *lk = lds_k[n & 1], *lv = lds_v[n & 1];
-            f32x16 s[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[h][r] = 0;
-#pragma unroll
-                for (int st = 0; st < kSteps; ++st) {
-                    const int at = (h * 32 + col) * D + (((2 * st + half) ^ (col & (kPieces - 1))) * 8);
-                    s[h] = T::mma32(*reinterpret_cast<const s16x8 *>(lk + at), qf[st], s[h]);
-                }
-            }
-            const int base = it.kv0 + n * kTileKv;
-            if (base + kTileKv > least) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (base + h * 32 + (r >> 2) * 8 + half * 4 + (r & 3) >= lim) s[h][r] = kNegInf;
-            }
-            float top = kNegInf;
+        }
+        const int base = it.kv0 + n * kTileKv;
+        if (base + kTileKv > least) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[h][r]);
-            top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
-            const float now = fmaxf(m, top), use = now == kNegInf ? 0.f : now;
-            if (__any(now != m)) {
-                const float f = exp2_of(m - use);
-                l *= f;
+                for (int r = 0; r < 16; ++r)
+                    if (base + h * 32 + (r >> 2) * 8 + half * 4 + (r & 3) >= lim) s[h][r] = kNegInf;
+        }
+        float top = kNegInf;
 #pragma unroll
-                for (int i = 0; i < kDb; ++i)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) o[i][r] *= f;
-                m = now;
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[h][r]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+        if (__any(top > m + kSlack)) {
+            const float now = fmaxf(m, top), f = now == kNegInf ? 1.f : exp2_of(m - now);
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < kDb; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[i][r] *= f;
+            m = now;
+        }
+        const float use = m == kNegInf ? 0.f : m;
+        s16x8 pf[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[h][r] = exp2_of(fmaf(s[h][r], a.scale_log2, -use));
+                l += s[h][r];
             }
-            s16x8 pf[4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int x = 0; x < 2; ++x) {
+                union { uint32_t u[4]; s16x8 v; } w;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[h][r] = exp2_of(fmaf(s[h][r], a.scale_log2, -use));
-                    l += s[h][r];
-                }
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    union { uint32_t u[4]; s16x8 v; } w;
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) w.u[y] = T::pack(s[h][8 * x + 2 * y], s[h][8 * x + 2 * y + 1]);
-                    pf[2 * h + x] = w.v;
-                }
-            }
-            const int quad = (lane >> 2) & 3, g16 = (lane >> 4) & 1;
-            const int vt = 4 * half + quad;     // token of this lane's address, within eight
-#pragma unroll
-            for (int i = 0; i < kDb; ++i) {
-                const int piece = (4 * i + 2 * g16 + ((lane & 3) >> 1)) ^ (2 * vt & (kPieces - 1));
-                const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
-#pragma unroll
-                for (int st = 0; st < 4; ++st)
-                    o[i] = T::mma32(join(read_tr(v + st * 16 * D), read_tr(v + (st * 16 + 8) * D)), pf[st], o[i]);
+                for (int y = 0; y < 4; ++y) w.u[y] = T::pack(s[h][8 * x + 2 * y], s[h][8 * x + 2 * y + 1]);
+                pf[2 * h + x] = w.v;
             }
         }
-        l += __shfl_xor(l, 32);
-        if (active) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            const float lse = l == 0.f ? kNegInf : m + log2_of(l);
-            if (it.part < 0) {
-                uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + hq * a.out_head + 4 * half;
+        const int quad = (lane >> 2) & 3, g16 = (lane >> 4) & 1;
+        const int vt = 4 * half + quad;     // token of this lane's address, within eight
 #pragma unroll
-                for (int i = 0; i < kDb; ++i)
+        for (int i = 0; i < kDb; ++i) {
+            const int piece = (4 * i + 2 * g16 + ((lane & 3) >> 1)) ^ (2 * vt & (kPieces - 1));
+            const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
 #pragma unroll
-                    for (int b = 0; b < 4; ++b)
-                        *reinterpret_cast<uint2 *>(to + 32 * i + 8 * b) =
-                            make_uint2(T::pack(o[i][4 * b] * inv, o[i][4 * b + 1] * inv),
-                                       T::pack(o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv));
-                if (a.lse_out && half == 0) a.lse_out[q_row * a.n_heads + hq] = lse * kLn2;
-            } else {
-                const int64_t at = it.part + (int64_t)tok * a.n_heads + hq;
-                float *to = a.ws.o + at * D + 4 * half;
+            for (int st = 0; st < 4; ++st)
+                o[i] = T::mma32(join(read_tr(v + st * 16 * D), read_tr(v + (st * 16 + 8) * D)), pf[st], o[i]);
+        }
+    }
+    l += __shfl_xor(l, 32);
+    if (active) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float lse = l == 0.f ? kNegInf : m + log2_of(l);
+        if (it.part < 0) {
+            uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + hq * a.out_head + 4 * half;
 #pragma unroll
-                for (int i = 0; i < kDb; ++i)
+            for (int i = 0; i < kDb; ++i)
 #pragma unroll
-                    for (int b = 0; b < 4; ++b)
-                        *reinterpret_cast<float4 *>(to + 32 * i + 8 * b) =
-                            make_float4(o[i][4 * b] * inv, o[i][4 * b + 1] * inv, o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv);
-                if (half == 0) a.ws.lse[at] = lse;
-            }
+                for (int b = 0; b < 4; ++b)
+                    *reinterpret_cast<uint2 *>(to + 32 * i + 8 * b) =
+                        make_uint2(T::pack(o[i][4 * b] * inv, o[i][4 * b + 1] * inv),
+                                   T::pack(o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv));
+            if (a.lse_out && half == 0) a.lse_out[q_row * a.n_heads + hq] = lse * kLn2;
+        } else {
+            const int64_t at = it.part + (int64_t)tok * a.n_heads + hq;
+            float *to = a.ws.o + at * D + 4 * half;
+#pragma unroll
+            for (int i = 0; i < kDb; ++i)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    *reinterpret_cast<float4 *>(to + 32 * i + 8 * b) =
+                        make_float4(o[i][4 * b] * inv, o[i][4 * b + 1] * inv, o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv);
+            if (half == 0) a.ws.lse[at] = lse;
         }
     }
 }
 
 // ------------------------------------------------------------------ narrow items
 
-// Up to 16 rows: a wave by itself, with 16 x 16 x 32 products and 32 tokens
-// (two pages) at a time.  K goes from memory to the registers that multiply it;
+// Up to 16 rows: a wave by itself, with 16 x 16 x 32 products and 64 tokens
+// (four pages) at a time.  K goes from memory to the registers that multiply it;
 // V through a piece of LDS of the wave's own, for the transposing read.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attn_narrow(AttnArgs a) {
-    constexpr int kPieces = D / 8, kSteps = D / 32, kDb = D / 16, kTok = 32;
-    __shared__ __align__(1024) uint16_t lds_v[4][kTok * D];
-    if (!a.ws.head->ok) return;
-    const int n_items = a.ws.head->n_narrow;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it, uint16_t *lv) {
+    constexpr int kPieces = D / 8, kSteps = D / 32, kDb = D / 16, kPages = kTileKv / kBlk;
+    const int lane = threadIdx.x & 63;
     const int col = lane & 15, quarter = lane >> 4;
     const uint16_t *zeros = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(a.ws.head) + kZeroOffset);
-    const uint16_t *kp = static_cast<const uint16_t *>(a.k), *vp = static_cast<const uint16_t *>(a.v);
-    uint16_t *lv = lds_v[wave];
-    for (int which = blockIdx.x * 4 + wave; which < n_items; which += gridDim.x * 4) {
-        const AttnItem it = a.ws.narrow[which];
-        const int head = it.head_tile & 255;
-        const int tok = col / a.group, hq = head * a.group + col - tok * a.group;
-        const bool active = tok < it.n_tok;
-        const int lim = active ? min(a.ws.lim[it.t0 + tok], it.kv1) : 0;
-        const int64_t q_row = active ? a.ws.tok[it.t0 + tok] : 0;
-        s16x8 qf[kSteps];
-        {
-            const uint16_t *q = static_cast<const uint16_t *>(a.q) + q_row * a.q_token + hq * a.q_head + quarter * 8;
+    const int head = it.head_tile & 255;
+    const uint16_t *kp = static_cast<const uint16_t *>(a.k) + (int64_t)head * a.head_stride;
+    const uint16_t *vp = static_cast<const uint16_t *>(a.v) + (int64_t)head * a.head_stride;
+    const int tok = col / a.group, hq = head * a.group + col - tok * a.group;
+    const bool active = tok < it.n_tok;
+    const int lim = active ? min(a.ws.lim[it.t0 + tok], it.kv1) : 0;
+    const int64_t q_row = active ? a.ws.tok[it.t0 + tok] : 0;
+    int most = lim;
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s)
-                qf[s] = active ? *reinterpret_cast<const s16x8 *>(q + 32 * s) : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    for (int d = 8; d; d >>= 1) most = max(most, __shfl_xor(most, d));
+    const int end = __builtin_amdgcn_readfirstlane(most);
+    const int32_t *table = a.table + (int64_t)it.seq * a.table_width;
+    int none;       // see wide_item
+    asm volatile("v_mov_b32 %0, 0" : "=v"(none));
+    int number[kPages];
+    auto look_up = [&](int base) {
+#pragma unroll
+        for (int h = 0; h < kPages; ++h) number[h] = table[min(base + h * kBlk, end - 1) / kBlk + none];
+    };
+    if (it.kv0 < end) look_up(it.kv0);
+    s16x8 qf[kSteps];
+    {
+        const uint16_t *q = static_cast<const uint16_t *>(a.q) + q_row * a.q_token + hq * a.q_head + quarter * 8;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+            qf[s] = active ? *reinterpret_cast<const s16x8 *>(q + 32 * s) : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    }
+    f32x4 o[kDb];
+#pragma unroll
+    for (int i = 0; i < kDb; ++i) o[i] = f32x4{0, 0, 0, 0};
+    float m = kNegInf, l = 0;
+    for (int base = it.kv0; base < end; base += kTileKv) {
+        s16x8 kf[kPages][kSteps];
+        int64_t from[kPages];
+#pragma unroll
+        for (int h = 0; h < kPages; ++h) {
+            const uint32_t page = min((uint32_t)__builtin_amdgcn_readfirstlane(number[h]), (uint32_t)(a.n_pages - 1));
+            from[h] = (int64_t)page * a.page_stride;
+            const uint16_t *k = kp + from[h] + col * a.token_stride + quarter * 8;
+#pragma unroll
+            for (int st = 0; st < kSteps; ++st) kf[h][st] = *reinterpret_cast<const s16x8 *>(k + 32 * st);
         }
-        int most = lim;
 #pragma unroll
-        for (int d = 8; d; d >>= 1) most = max(most, __shfl_xor(most, d));
-        const int end = __builtin_amdgcn_readfirstlane(most);
-        const int32_t *table = a.table + (int64_t)it.seq * a.table_width;
-        f32x4 o[kDb];
+        for (int h = 0; h < kPages; ++h)
 #pragma unroll
-        for (int i = 0; i < kDb; ++i) o[i] = f32x4{0, 0, 0, 0};
-        float m = kNegInf, l = 0;
-        for (int base = it.kv0; base < end; base += kTok) {
-            f32x4 s[2];
-            s16x8 kf[2][kSteps];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int t_first = base + h * kBlk;
-                const uint32_t page = min((uint32_t)table[min(t_first, end - 1) / kBlk], (uint32_t)(a.n_pages - 1));
-                const int64_t from = (int64_t)page * a.page_stride + (int64_t)head * a.head_stride;
-                const uint16_t *k = kp + from + col * a.token_stride + quarter * 8;
-#pragma unroll
-                for (int st = 0; st < kSteps; ++st) kf[h][st] = *reinterpret_cast<const s16x8 *>(k + 32 * st);
-#pragma unroll
-                for (int i = 0; i < kPieces / 4; ++i) {
-                    const int u = i * 64 + lane, t = u / kPieces, c = u % kPieces;
-                    const uint16_t *v = vp + from + t * a.token_stride + (c ^ (2 * t & (kPieces - 1))) * 8;
-                    load_lds16(t_first + t < end ? v : zeros, lv + h * kBlk * D + i * 512);
-                }
+            for (int i = 0; i < kPieces / 4; ++i) {
+                const int u = i * 64 + lane, t = u / kPieces, c = u % kPieces;
+                const uint16_t *v = vp + from[h] + t * a.token_stride + (c ^ (2 * t & (kPieces - 1))) * 8;
+                load_lds16(base + h * kBlk + t < end ? v : zeros, lv + h * kBlk * D + i * 512);
             }
+        if (base + kTileKv < end) look_up(base + kTileKv);
+        f32x4 s[kPages];
+        float top = kNegInf;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                s[h] = f32x4{0, 0, 0, 0};
+        for (int h = 0; h < kPages; ++h) {
+            s[h] = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int st = 0; st < kSteps; ++st) s[h] = T::mma16(kf[h][st], qf[st], s[h]);
-            }
-            float top = kNegInf;
+            for (int st = 0; st < kSteps; ++st) s[h] = T::mma16(kf[h][st], qf[st], s[h]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (base + h * kBlk + quarter * 4 + r >= lim) s[h][r] = kNegInf;
-                    top = fmaxf(top, s[h][r]);
-                }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
-            const float now = fmaxf(m, top), use = now == kNegInf ? 0.f : now;
-            if (__any(now != m)) {
-                const float f = exp2_of(m - use);
-                l *= f;
-#pragma unroll
-                for (int i = 0; i < kDb; ++i) o[i] *= f;
-                m = now;
-            }
-            union { uint32_t u[4]; s16x8 v; } w;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[h][r] = exp2_of(fmaf(s[h][r], a.scale_log2, -use));
-                    l += s[h][r];
-                }
-                w.u[2 * h] = T::pack(s[h][0], s[h][1]);
-                w.u[2 * h + 1] = T::pack(s[h][2], s[h][3]);
-            }
-            wait_loads();
-            const int vt = 4 * quarter + ((lane >> 2) & 3);     // token of this lane's address, within a page
-#pragma unroll
-            for (int i = 0; i < kDb; ++i) {
-                const int piece = (2 * i + ((lane & 3) >> 1)) ^ (2 * vt & (kPieces - 1));
-                const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
-                o[i] = T::mma16(join(read_tr(v), read_tr(v + kBlk * D)), w.v, o[i]);
-            }
-            // the reads are done before the next tokens land in the same place
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        }
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        if (active) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            const float lse = l == 0.f ? kNegInf : m + log2_of(l);
-            if (it.part < 0) {
-                uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + hq * a.out_head + 4 * quarter;
-#pragma unroll
-                for (int i = 0; i < kDb; ++i)
-                    *reinterpret_cast<uint2 *>(to + 16 * i) = make_uint2(T::pack(o[i][0] * inv, o[i][1] * inv),
-                                                                         T::pack(o[i][2] * inv, o[i][3] * inv));
-                if (a.lse_out && quarter == 0) a.lse_out[q_row * a.n_heads + hq] = lse * kLn2;
-            } else {
-                const int64_t at = it.part + (int64_t)tok * a.n_heads + hq;
-                float *to = a.ws.o + at * D + 4 * quarter;
-#pragma unroll
-                for (int i = 0; i < kDb; ++i)
-                    *reinterpret_cast<float4 *>(to + 16 * i) =
-                        make_float4(o[i][0] * inv, o[i][1] * inv, o[i][2] * inv, o[i][3] * inv);
-                if (quarter == 0) a.ws.lse[at] = lse;
+            for (int r = 0; r < 4; ++r) {
+                if (base + h * kBlk + quarter * 4 + r >= lim) s[h][r] = kNegInf;
+                top = fmaxf(top, s[h][r]);
             }
         }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+        if (__any(top > m + kSlack)) {
+            const float now = fmaxf(m, top), f = now == kNegInf ? 1.f : exp2_of(m - now);
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < kDb; ++i) o[i] *= f;
+            m = now;
+        }
+        const float use = m == kNegInf ? 0.f : m;
+        union { uint32_t u[2 * kPages]; s16x8 v[kPages / 2]; } w;
+#pragma unroll
+        for (int h = 0; h < kPages; ++h) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[h][r] = exp2_of(fmaf(s[h][r], a.scale_log2, -use));
+                l += s[h][r];
+            }
+            w.u[2 * h] = T::pack(s[h][0], s[h][1]);
+            w.u[2 * h + 1] = T::pack(s[h][2], s[h][3]);
+        }
+        wait_loads();
+        const int vt = 4 * quarter + ((lane >> 2) & 3);     // token of this lane's address, within a page
+#pragma unroll
+        for (int i = 0; i < kDb; ++i) {
+            const int piece = (2 * i + ((lane & 3) >> 1)) ^ (2 * vt & (kPieces - 1));
+            const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
+#pragma unroll
+            for (int h = 0; h < kPages; h += 2)
+                o[i] = T::mma16(join(read_tr(v + h * kBlk * D), read_tr(v + (h + 1) * kBlk * D)), w.v[h / 2], o[i]);
+        }
+        // the reads are done before the next tokens land in the same place
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (active) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float lse = l == 0.f ? kNegInf : m + log2_of(l);
+        if (it.part < 0) {
+            uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + hq * a.out_head + 4 * quarter;
+#pragma unroll
+            for (int i = 0; i < kDb; ++i)
+                *reinterpret_cast<uint2 *>(to + 16 * i) = make_uint2(T::pack(o[i][0] * inv, o[i][1] * inv),
+                                                                     T::pack(o[i][2] * inv, o[i][3] * inv));
+            if (a.lse_out && quarter == 0) a.lse_out[q_row * a.n_heads + hq] = lse * kLn2;
+        } else {
+            const int64_t at = it.part + (int64_t)tok * a.n_heads + hq;
+            float *to = a.ws.o + at * D + 4 * quarter;
+#pragma unroll
+            for (int i = 0; i < kDb; ++i)
+                *reinterpret_cast<float4 *>(to + 16 * i) =
+                    make_float4(o[i][0] * inv, o[i][1] * inv, o[i][2] * inv, o[i][3] * inv);
+            if (quarter == 0) a.ws.lse[at] = lse;
+        }
+    }
+}
+
+// ------------------------------------------------------------------ items
+
+// Wide items are bound by the matrix units and LDS, narrow ones by memory: of
+// the two workgroups on a CU one begins with the wide list and one with the
+// narrow one, so that both kinds run side by side.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void attn_items(AttnArgs a) {
+    __shared__ __align__(1024) uint16_t lds[4 * kTileKv * D];
+    __shared__ int lds_lim[4];
+    if (!a.ws.head->ok) return;
+    const int n_wide = a.ws.head->n_wide, n_narrow = a.ws.head->n_narrow;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool wide_first = blockIdx.x < gridDim.x / 2;
+    for (int phase = 0; phase < 2; ++phase) {
+        if ((phase == 0) == wide_first) {
+            for (int turn = blockIdx.x; turn < xcd_turns(n_wide); turn += gridDim.x) {
+                const int which = xcd_item(turn, n_wide);
+                if (which >= 0) wide_item<T, D>(a, a.ws.wide[which], lds, lds_lim);
+            }
+        } else {
+            for (int which = blockIdx.x + wave * gridDim.x; which < n_narrow; which += gridDim.x * 4)
+                narrow_item<T, D>(a, a.ws.narrow[which], lds + wave * kTileKv * D);
+        }
+        __syncthreads();
     }
 }
 
 // ------------------------------------------------------------------ join
 
-// A wave for each (query, head): its parts by their sums of exponentials.
-template <typename T, int D>
+// A wave for kHeads heads of a query.  A lane weighs one part of one head, 64 /
+// kHeads parts at a time; the parts' values follow with 16 loads in flight.
+template <typename T, int D, int kHeads>
 __global__ __launch_bounds__(256) void attn_join(AttnArgs a, int32_t n_req) {
+    constexpr int kParts = 64 / kHeads, kFly = 16 / kHeads, kPer = D / 64;
     if (!a.ws.head->ok) return;
-    const int lane = threadIdx.x & 63;
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t t = at / a.n_heads;
-    const int h = (int)(at - t * a.n_heads);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int per_query = (a.n_heads + kHeads - 1) / kHeads;
+    const int64_t at = (int64_t)blockIdx.x * 4 + wave;
+    const int64_t t = at / per_query;
+    const int h0 = (int)(at - t * per_query) * kHeads;
     if (t >= a.n_tokens) return;
+    const int64_t q_row = a.ws.tok[t];
     const int j = a.ws.pos[t];
     const AttnParts own = a.ws.parts[j], grp = a.ws.parts[n_req + j];
     if (own.chunks < 0) return;     // written already
-    const int n = own.chunks + grp.chunks;
-    auto row = [&](int c) -> int64_t {
+    const int n = own.chunks + grp.chunks, heads = min(a.n_heads - h0, kHeads);
+    auto row = [&](int c) -> int64_t {      // of head h0
         const AttnParts &x = c < grp.chunks ? grp : own;
         const int k = c < grp.chunks ? c : c - grp.chunks;
-        return x.base + ((int64_t)k * x.n_tok + (t - x.t0)) * a.n_heads + h;
+        return x.base + ((int64_t)k * x.n_tok + (t - x.t0)) * a.n_heads + h0;
     };
-    // a lane holds one part's weight; the parts' values follow with all loads of four in flight
-    float top = kNegInf, sum = 0, o[2] = {0, 0};
-    for (int c0 = 0; c0 < n; c0 += 64) {
-        const int c = c0 + lane;
-        const int64_t r = c < n ? row(c) : 0;
-        const float lse = c < n ? a.ws.lse[r] : kNegInf;
+    const int my_head = lane / kParts, my_part = lane % kParts;
+    float top = kNegInf, sum = 0, o[kHeads][kPer];
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h)
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[h][e] = 0;
+    for (int c0 = 0; c0 < n; c0 += kParts) {
+        const int c = c0 + my_part;
+        const float lse = c < n && my_head < heads ? a.ws.lse[row(c) + my_head] : kNegInf;
         float now = fmaxf(top, lse);
 #pragma unroll
-        for (int d = 32; d; d >>= 1) now = fmaxf(now, __shfl_xor(now, d));
-        if (now == kNegInf) continue;
-        const float f = exp2_of(top - now);
-        const float w = exp2_of(lse - now);
+        for (int d = kParts / 2; d; d >>= 1) now = fmaxf(now, __shfl_xor(now, d));
+        const float use = now == kNegInf ? 0.f : now;
+        const float f = exp2_of(top - use), w = exp2_of(lse - use);
         float all = w;
 #pragma unroll
-        for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d);
+        for (int d = kParts / 2; d; d >>= 1) all += __shfl_xor(all, d);
         sum = sum * f + all;
-        o[0] *= f;
-        o[1] *= f;
         top = now;
-        const int m = min(n - c0, 64);
-        for (int k0 = 0; k0 < m; k0 += 8) {
-            float x[8][2], wk[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                // the values of an empty part are not written: its weight is 0
-                const int from = min(k0 + k, m - 1);
-                wk[k] = k0 + k < m ? __shfl(w, from) : 0.f;
-                const int64_t rk = ((int64_t)__shfl((int)(r >> 32), from) << 32) | (uint32_t)__shfl((int)r, from);
-                if (D == 128) {
-                    const float2 v = *reinterpret_cast<const float2 *>(a.ws.o + rk * D + 2 * lane);
-                    x[k][0] = v.x;
-                    x[k][1] = v.y;
-                } else {
-                    x[k][0] = a.ws.o[rk * D + lane];
-                    x[k][1] = 0;
+        for (int h = 0; h < kHeads; ++h) {
+            const float fh = __shfl(f, h * kParts);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) o[h][e] *= fh;
+        }
+        const int m = min(n - c0, kParts);
+        for (int k0 = 0; k0 < m; k0 += kFly) {
+            float x[kFly][kHeads][kPer];
+#pragma unroll
+            for (int k = 0; k < kFly; ++k) {
+                const float *from = a.ws.o + row(c0 + min(k0 + k, m - 1)) * D + kPer * lane;
+#pragma unroll
+                for (int h = 0; h < kHeads; ++h)
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) x[k][h][e] = from[min(h, heads - 1) * D + e];
+            }
+#pragma unroll
+            for (int k = 0; k < kFly; ++k)
+#pragma unroll
+                for (int h = 0; h < kHeads; ++h) {
+                    // a part without tokens has no values, and the weight 0
+                    const float wk = k0 + k < m ? __shfl(w, h * kParts + k0 + k) : 0.f;
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) o[h][e] += wk == 0.f ? 0.f : wk * x[k][h][e];
                 }
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                o[0] += wk[k] == 0.f ? 0.f : wk[k] * x[k][0];
-                o[1] += wk[k] == 0.f ? 0.f : wk[k] * x[k][1];
-            }
         }
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int64_t q_row = a.ws.tok[t];
-    uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + h * a.out_head;
-    if (D == 128) *reinterpret_cast<uint32_t *>(to + 2 * lane) = T::pack(o[0] * inv, o[1] * inv);
-    else to[lane] = (uint16_t)T::pack(o[0] * inv, 0.f);
-    if (a.lse_out && lane == 0) a.lse_out[q_row * a.n_heads + h] = sum == 0.f ? kNegInf : (top + log2_of(sum)) * kLn2;
+    const float joined = sum == 0.f ? kNegInf : (top + log2_of(sum)) * kLn2;
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+        const float ih = __shfl(inv, h * kParts);
+        if (h >= heads) continue;
+        uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + (h0 + h) * a.out_head;
+        if (kPer == 2) *reinterpret_cast<uint32_t *>(to + 2 * lane) = T::pack(o[h][0] * ih, o[h][kPer - 1] * ih);
+        else to[lane] = (uint16_t)T::pack(o[h][0] * ih, 0.f);
+    }
+    if (a.lse_out && my_part == 0 && my_head < heads) a.lse_out[q_row * a.n_heads + h0 + my_head] = joined;
 }
 
 template <typename T, int D>
 hipError_t launch(const AttnArgs &a, int32_t n_req, hipStream_t st) {
-    attn_wide<T, D><<<512, 256, 0, st>>>(a);
-    attn_narrow<T, D><<<1024, 256, 0, st>>>(a);
-    const int64_t rows = a.n_tokens * a.n_heads;
-    attn_join<T, D><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a, n_req);
+    attn_items<T, D><<<512, 256, 0, st>>>(a);     // two workgroups to a CU
+    // A wave to a row where that does no more than fill the chip; where there are many rows, mostly
+    // of two parts, four rows to a wave have more loads in flight.
+    const int64_t rows = a.n_tokens * a.n_heads, waves = a.n_tokens * ((a.n_heads + 3) / 4);
+    if (rows <= 16384) attn_join<T, D, 1><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a, n_req);
+    else attn_join<T, D, 4><<<(uint32_t)((waves + 3) / 4), 256, 0, st>>>(a, n_req);
     return hipGetLastError();
 }
 
@@ -748,13 +822,18 @@ int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_h
 }
 
 hipError_t launch_attn_plan(const AttnPlanArgs &a, hipStream_t st) {
-    const size_t bytes = 4 * (7 * (size_t)a.n_req + 2);
-    if (bytes > 16 * 1024) {    // beside the kernel's own 48 KiB
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_plan),
+    const size_t bytes = 4 * (7 * (size_t)a.n_req + 3);
+    // a barrier and a sum over 16 wavefronts cost more than what few requests have to do
+    if (a.n_req <= 256) {
+        attn_plan<256><<<kPlanGroups, 256, bytes, st>>>(a);
+        return hipGetLastError();
+    }
+    if (bytes > 16 * 1024) {    // beside the kernel's own 42 KB
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_plan<1024>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != hipSuccess) return e;
     }
-    attn_plan<<<1, kPlanThreads, bytes, st>>>(a);
+    attn_plan<1024><<<kPlanGroups, 1024, bytes, st>>>(a);
     return hipGetLastError();
 }
 
