@@ -194,13 +194,15 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
     __shared__ int32_t first_item[NT];
     __shared__ int32_t lds[3 * (NT / 64)];
     __shared__ int64_t lds64[2 * (NT / 64)];
-    __shared__ int any_bad, stop;
+    constexpr int kSmallGroup = 16;
+    __shared__ int large[PC_MAX_BATCH / kSmallGroup];
+    __shared__ int any_bad, stop, n_large;
     __shared__ uint32_t seen[PC_MAX_BATCH / 32];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool grouped = a.order != nullptr, first = blockIdx.x == 0;
     const int wg_tid = blockIdx.x * NT + tid, wg_step = gridDim.x * NT;     // of what the workgroups share
     if (tid < PC_MAX_BATCH / 32) seen[tid] = 0;
-    if (tid == 0) any_bad = 0;
+    if (tid == 0) any_bad = n_large = 0;
     if (first && tid < 64) reinterpret_cast<int32_t *>(ws.head)[tid] = 0;
     __syncthreads();
     // all that the caller gives, at once
@@ -255,15 +257,32 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
         ws.lim[t] = a.causal ? len[r] - n + i + 1 : len[r];
         ws.pos[t] = j;
     }
-    // the tokens that all members of a group share: a wave for each group
-    for (int g = wave; g < n_groups; g += NT / 64) {
-        const int j0 = goff[g], j1 = goff[g + 1], blocks = share[g];
+    // the tokens that all members of a group share: by a thread for small groups, a wave for others
+    auto shared_tokens = [&](int g, int least) {
+        const int64_t tokens = least / kBlk * kBlk, blocks = share[g];
+        return blocks <= 0 ? 0 : (int)min(tokens, blocks * kBlk);
+    };
+    for (int g = tid; g < n_groups; g += NT) {
+        const int j0 = goff[g], j1 = goff[g + 1];
+        if (j1 - j0 > kSmallGroup) {
+            large[atomicAdd(&n_large, 1)] = g;
+            continue;
+        }
+        int least = 0x7fffffff;
+        for (int j = j0; j < j1; ++j) least = min(least, len[request(j)]);
+        const int tokens = j1 - j0 < 2 ? 0 : shared_tokens(g, least);
+        if (tokens)
+            for (int j = j0; j < j1; ++j) place[j] = request(j) | g << 16;
+        share[g] = tokens;
+    }
+    __syncthreads();
+    for (int i = wave; i < n_large; i += NT / 64) {
+        const int g = large[i], j0 = goff[g], j1 = goff[g + 1];
         int least = 0x7fffffff;
         for (int j = j0 + lane; j < j1; j += 64) least = min(least, len[request(j)]);
 #pragma unroll
         for (int d = 32; d; d >>= 1) least = min(least, __shfl_xor(least, d));
-        int tokens = j1 - j0 < 2 || blocks <= 0 ? 0 : least / kBlk * kBlk;
-        if ((int64_t)blocks * kBlk < tokens) tokens = blocks * kBlk;
+        const int tokens = shared_tokens(g, least);
         if (tokens)
             for (int j = j0 + lane; j < j1; j += 64) place[j] = request(j) | g << 16;
         if (lane == 0) share[g] = tokens;
@@ -442,6 +461,9 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
         }
         const uint16_t *lk = lds + (n & 1) * kBuf, *lv = lk + 2 * kBuf;
         f32x16 s[2];
+        // the wave that multiplies goes before the one that weighs (3.5 % less time on long prompts;
+        // the same around the second product costs 3 %)
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -452,6 +474,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
                 s[h] = T::mma32(*reinterpret_cast<const s16x8 *>(lk + at), qf[st], s[h]);
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         const int base = it.kv0 + n * kTileKv;
         if (base + kTileKv > least) {
 #pragma unroll
