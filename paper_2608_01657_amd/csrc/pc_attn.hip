@@ -556,26 +556,18 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
 
 // ------------------------------------------------------------------ narrow items
 
-// Up to 16 rows: a wave by itself, with 16 x 16 x 32 products and 64 tokens
-// (four pages) at a time.  K goes from memory to the registers that multiply it;
-// V through a piece of LDS of the wave's own, for the transposing read.
+// Up to 16 rows: a wave by itself, with 16 x 16 x 32 products and 32 tokens
+// (two pages) at a time, bound by memory.  K and V of the next tokens are
+// loaded to registers while the present ones are weighed and multiplied; V
+// goes on through a piece of LDS of the wave's own, for the transposing read.
 template <typename T, int D>
 __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it, uint16_t *lv) {
-    constexpr int kPieces = D / 8, kSteps = D / 32, kDb = D / 16, kPages = kTileKv / kBlk;
+    constexpr int kPieces = D / 8, kSteps = D / 32, kDb = D / 16, kStep = 32, kPages = kStep / kBlk;
     const int lane = threadIdx.x & 63;
     const int col = lane & 15, quarter = lane >> 4;
-    const uint16_t *zeros = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(a.ws.head) + kZeroOffset);
-    const int head = it.head_tile & 255;
+    const int head = it.head_tile & 255, end = it.kv1;
     const uint16_t *kp = static_cast<const uint16_t *>(a.k) + (int64_t)head * a.head_stride;
     const uint16_t *vp = static_cast<const uint16_t *>(a.v) + (int64_t)head * a.head_stride;
-    const int tok = col / a.group, hq = head * a.group + col - tok * a.group;
-    const bool active = tok < it.n_tok;
-    const int lim = active ? min(a.ws.lim[it.t0 + tok], it.kv1) : 0;
-    const int64_t q_row = active ? a.ws.tok[it.t0 + tok] : 0;
-    int most = lim;
-#pragma unroll
-    for (int d = 8; d; d >>= 1) most = max(most, __shfl_xor(most, d));
-    const int end = __builtin_amdgcn_readfirstlane(most);
     const int32_t *table = a.table + (int64_t)it.seq * a.table_width;
     int none;       // see wide_item
     asm volatile("v_mov_b32 %0, 0" : "=v"(none));
@@ -584,7 +576,27 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
 #pragma unroll
         for (int h = 0; h < kPages; ++h) number[h] = table[min(base + h * kBlk, end - 1) / kBlk + none];
     };
-    if (it.kv0 < end) look_up(it.kv0);
+    const int k_at = col * a.token_stride + quarter * 8, v_at = lane / kPieces * a.token_stride + lane % kPieces * 8,
+              v_step = 64 / kPieces * a.token_stride;
+    s16x8 kf[kPages][kSteps], vf[kPages][kSteps];
+    auto load = [&](int base) {
+#pragma unroll
+        for (int h = 0; h < kPages; ++h) {
+            const uint32_t page = min((uint32_t)__builtin_amdgcn_readfirstlane(number[h]), (uint32_t)(a.n_pages - 1));
+            const uint16_t *k = kp + (int64_t)page * a.page_stride, *v = vp + (int64_t)page * a.page_stride;
+#pragma unroll
+            for (int st = 0; st < kSteps; ++st) kf[h][st] = *reinterpret_cast<const s16x8 *>(k + k_at + 32 * st);
+#pragma unroll
+            for (int st = 0; st < kSteps; ++st) vf[h][st] = *reinterpret_cast<const s16x8 *>(v + v_at + st * v_step);
+        }
+        if (base + kStep < end) look_up(base + kStep);
+    };
+    look_up(it.kv0);
+    load(it.kv0);
+    const int tok = col / a.group, hq = head * a.group + col - tok * a.group;
+    const bool active = tok < it.n_tok;
+    const int lim = active ? min(a.ws.lim[it.t0 + tok], it.kv1) : 0;
+    const int64_t q_row = active ? a.ws.tok[it.t0 + tok] : 0;
     s16x8 qf[kSteps];
     {
         const uint16_t *q = static_cast<const uint16_t *>(a.q) + q_row * a.q_token + hq * a.q_head + quarter * 8;
@@ -596,39 +608,36 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
 #pragma unroll
     for (int i = 0; i < kDb; ++i) o[i] = f32x4{0, 0, 0, 0};
     float m = kNegInf, l = 0;
-    for (int base = it.kv0; base < end; base += kTileKv) {
-        s16x8 kf[kPages][kSteps];
-        int64_t from[kPages];
-#pragma unroll
-        for (int h = 0; h < kPages; ++h) {
-            const uint32_t page = min((uint32_t)__builtin_amdgcn_readfirstlane(number[h]), (uint32_t)(a.n_pages - 1));
-            from[h] = (int64_t)page * a.page_stride;
-            const uint16_t *k = kp + from[h] + col * a.token_stride + quarter * 8;
-#pragma unroll
-            for (int st = 0; st < kSteps; ++st) kf[h][st] = *reinterpret_cast<const s16x8 *>(k + 32 * st);
-        }
+    for (int base = it.kv0; base < end; base += kStep) {
+        // V to LDS, a token's pieces permuted as in wide_item.  A wave's LDS operations stay in order, so
+        // the last tokens' reads are done.  Behind the end there may be anything, and zero times anything
+        // is to be zero.
+        const bool whole = base + kStep <= end;
 #pragma unroll
         for (int h = 0; h < kPages; ++h)
 #pragma unroll
-            for (int i = 0; i < kPieces / 4; ++i) {
-                const int u = i * 64 + lane, t = u / kPieces, c = u % kPieces;
-                const uint16_t *v = vp + from[h] + t * a.token_stride + (c ^ (2 * t & (kPieces - 1))) * 8;
-                load_lds16(base + h * kBlk + t < end ? v : zeros, lv + h * kBlk * D + i * 512);
+            for (int st = 0; st < kSteps; ++st) {
+                const int u = st * 64 + lane, t = u / kPieces, c = u % kPieces;
+                s16x8 v = vf[h][st];
+                if (!whole && base + h * kBlk + t >= end) v = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                *reinterpret_cast<s16x8 *>(lv + (h * kBlk + t) * D + (c ^ (2 * t & (kPieces - 1))) * 8) = v;
             }
-        if (base + kTileKv < end) look_up(base + kTileKv);
         f32x4 s[kPages];
-        float top = kNegInf;
 #pragma unroll
         for (int h = 0; h < kPages; ++h) {
             s[h] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int st = 0; st < kSteps; ++st) s[h] = T::mma16(kf[h][st], qf[st], s[h]);
+        }
+        if (base + kStep < end) load(base + kStep);
+        float top = kNegInf;
+#pragma unroll
+        for (int h = 0; h < kPages; ++h)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 if (base + h * kBlk + quarter * 4 + r >= lim) s[h][r] = kNegInf;
                 top = fmaxf(top, s[h][r]);
             }
-        }
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
         if (__any(top > m + kSlack)) {
@@ -650,7 +659,6 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
             w.u[2 * h] = T::pack(s[h][0], s[h][1]);
             w.u[2 * h + 1] = T::pack(s[h][2], s[h][3]);
         }
-        wait_loads();
         const int vt = 4 * quarter + ((lane >> 2) & 3);     // token of this lane's address, within a page
 #pragma unroll
         for (int i = 0; i < kDb; ++i) {
@@ -660,8 +668,6 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
             for (int h = 0; h < kPages; h += 2)
                 o[i] = T::mma16(join(read_tr(v + h * kBlk * D), read_tr(v + (h + 1) * kBlk * D)), w.v[h / 2], o[i]);
         }
-        // the reads are done before the next tokens land in the same place
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);

@@ -49,7 +49,7 @@ constexpr int kWideRows = 128;       // query rows of a wide tile
 constexpr int kNarrowRows = 16;      // query rows of a narrow tile
 // Items that the plan aims at where it splits a long axis, and the fewest
 // 64-token blocks of an item that it splits down to.
-constexpr int kWideItems = 512, kNarrowItems = 2048;
+constexpr int kWideItems = 256, kNarrowItems = 1024;
 constexpr int kWideMinBlocks = 4, kNarrowMinBlocks = 2;
 
 // One piece of work: a tile of query rows of one KV head against a range of
