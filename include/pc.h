@@ -292,7 +292,7 @@ enum { PC_HEADS_FIRST = 0,            /* a page is [n_kv_heads][16][head_dim]   
 
 #define PC_MAX_SEQS 262144            /* sequences of a pool                           */
 #define PC_MAX_POOL_PAGES (1 << 27)
-#define PC_MAX_BATCH 4096             /* requests of one batch                         */
+#define PC_MAX_BATCH 4096             /* requests of one batch, sequences that grow at once */
 
 typedef struct {
     void *d_k, *d_v;                  /* page 0 of layer 0, 16-byte aligned            */
@@ -332,7 +332,8 @@ int64_t pc_pages_workspace_bytes(const pc_pages *pages, int64_t n);
 int32_t pc_pages_fork(const pc_pages *pages, const int32_t *d_parent, const int32_t *d_child, int32_t n,
                       int32_t *d_status, void *stream);
 
-/* Sequence d_seq[i] grows by d_add[i] >= 0 tokens; the sequences are distinct.
+/* Sequence d_seq[i] grows by d_add[i] >= 0 tokens; the sequences are distinct,
+ * PC_MAX_BATCH of them at most (else PC_EUNSUPPORTED).
  * New pages are the lowest that nobody holds, handed out in the order of the
  * list.  A last page that is filled in part and held by others too is copied
  * for a sequence that grows, K and V of every layer, the copy taking the first

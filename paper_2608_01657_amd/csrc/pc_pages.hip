@@ -23,24 +23,26 @@ __device__ __forceinline__ bool len_ok(const pc_pages &p, int len) {
     return len >= 0 && (int64_t)len <= (int64_t)p.table_width * kBlk;
 }
 
-// Exclusive sum over the workgroup's threads; *total: over all of them.
-template <typename N>
+// Exclusive sum over the workgroup's NT threads; *total: over all of them.
+template <int NT, typename N>
 __device__ N block_sum(N v, N *total, N *lds) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     N x = v;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const N y = __shfl_up(x, d);
-        if (lane >= d) x += y;
+        x += lane >= d ? y : 0;
     }
     __syncthreads();
     if (lane == 63) lds[w] = x;
     __syncthreads();
-    N before = 0, all = 0;
-    for (int i = 0; i < nw; ++i) {
-        const N t = lds[i];
-        if (i < w) before += t;
-        all += t;
+    N t[NT / 64], before = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) t[i] = lds[i];
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) {
+        before += i < w ? t[i] : 0;
+        all += t[i];
     }
     *total = all;
     return before + x - v;
@@ -85,60 +87,101 @@ __device__ __forceinline__ void copy_page(const pc_pages &p, int which, int src,
 
 // ------------------------------------------------------------------ fork, free
 
+// Whether the lists are as they should be (child == nullptr: that of
+// pc_pages_free).  One workgroup, all of its threads; a thread's own answer.
+__device__ bool bad_lists(const pc_pages &p, const int32_t *seq, const int32_t *child, int32_t n, uint32_t *seen) {
+    bool bad = bad_list(p, child ? child : seq, n, seen);
+    if (child)
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+            const uint32_t s = (uint32_t)seq[i], c = (uint32_t)child[i];
+            bad |= s >= (uint32_t)p.n_seqs || (seen[s >> 5] >> (s & 31) & 1);
+            bad |= c >= (uint32_t)p.n_seqs || p.d_len[c] != 0;
+        }
+    return bad;
+}
+
+// Whether sequence s's length and page numbers are in range, by `step` threads
+// that begin at `at`; false where s is not in the pool (bad_lists says so).
+__device__ bool bad_pages(const pc_pages &p, uint32_t s, int at, int step) {
+    if (s >= (uint32_t)p.n_seqs) return false;
+    const int len = p.d_len[s];
+    if (!len_ok(p, len)) return true;
+    const int32_t *row = p.d_table + (int64_t)s * p.table_width;
+    const int nb = blocks_of(len);
+    bool bad = false;
+    for (int i = at; i < nb; i += step) bad |= !page_ok(p, row[i]);
+    return bad;
+}
+
+__device__ void fork_one(const pc_pages &p, int64_t from, int64_t to, int at, int step) {
+    const int len = p.d_len[from], nb = blocks_of(len);
+    const int32_t *src = p.d_table + from * p.table_width;
+    int32_t *dst = p.d_table + to * p.table_width;
+    for (int i = at; i < nb; i += step) {
+        const int page = src[i];
+        dst[i] = page;
+        atomicAdd(&p.d_refs[page], 1);
+    }
+    if (at == 0) p.d_len[to] = len;
+}
+
+__device__ void free_one(const pc_pages &p, int64_t s, int len, int at, int step) {
+    const int32_t *row = p.d_table + s * p.table_width;
+    const int nb = blocks_of(len);
+    for (int i = at; i < nb; i += step) atomicSub(&p.d_refs[row[i]], 1);
+}
+
 // Workgroup 0 looks at the lists, the others each at one sequence's pages.
-// children == nullptr: the list of pc_pages_free.
-__global__ __launch_bounds__(kThreads) void check_lists(pc_pages p, const int32_t *seq, const int32_t *child, int32_t n,
-                                                        int32_t *status) {
+__global__ __launch_bounds__(256) void check_lists(pc_pages p, const int32_t *seq, const int32_t *child, int32_t n,
+                                                   int32_t *status) {
     if (stopped(status)) return;
     extern __shared__ uint32_t seen[];
-    bool bad = false;
-    if (blockIdx.x == 0) {
-        bad = bad_list(p, child ? child : seq, n, seen);
-        if (child)
-            for (int i = threadIdx.x; i < n; i += kThreads) {
-                const uint32_t s = (uint32_t)seq[i], c = (uint32_t)child[i];
-                bad |= s >= (uint32_t)p.n_seqs || (seen[s >> 5] >> (s & 31) & 1);
-                bad |= c >= (uint32_t)p.n_seqs || p.d_len[c] != 0;
-            }
-    } else {
-        const uint32_t s = (uint32_t)seq[blockIdx.x - 1];
-        if (s < (uint32_t)p.n_seqs) {
-            const int len = p.d_len[s];
-            if (!len_ok(p, len)) {
-                bad = true;
-            } else {
-                const int32_t *row = p.d_table + (int64_t)s * p.table_width;
-                const int nb = blocks_of(len);
-                for (int i = threadIdx.x; i < nb; i += kThreads) bad |= !page_ok(p, row[i]);
-            }
-        }
-    }
+    const bool bad = blockIdx.x == 0 ? bad_lists(p, seq, child, n, seen)
+                                     : bad_pages(p, (uint32_t)seq[blockIdx.x - 1], threadIdx.x, blockDim.x);
     if (bad) atomicExch(status, PC_EINVAL);
 }
 
 __global__ __launch_bounds__(256) void fork_pages(pc_pages p, const int32_t *parent, const int32_t *child,
                                                   const int32_t *status) {
     if (*status != PC_OK) return;
-    const int64_t from = parent[blockIdx.x], to = child[blockIdx.x];
-    const int len = p.d_len[from], nb = blocks_of(len);
-    const int32_t *src = p.d_table + from * p.table_width;
-    int32_t *dst = p.d_table + to * p.table_width;
-    for (int i = threadIdx.x; i < nb; i += blockDim.x) {
-        const int page = src[i];
-        dst[i] = page;
-        atomicAdd(&p.d_refs[page], 1);
-    }
-    if (threadIdx.x == 0) p.d_len[to] = len;
+    fork_one(p, parent[blockIdx.x], child[blockIdx.x], threadIdx.x, blockDim.x);
 }
 
 __global__ __launch_bounds__(256) void free_pages(pc_pages p, const int32_t *seq, const int32_t *status) {
     if (*status != PC_OK) return;
     const int64_t s = seq[blockIdx.x];
-    const int nb = blocks_of(p.d_len[s]);
-    const int32_t *row = p.d_table + s * p.table_width;
-    for (int i = threadIdx.x; i < nb; i += blockDim.x) atomicSub(&p.d_refs[row[i]], 1);
-    __syncthreads();
+    const int len = p.d_len[s];
+    __syncthreads();        // all have read it
+    free_one(p, s, len, threadIdx.x, blockDim.x);
     if (threadIdx.x == 0) p.d_len[s] = 0;
+}
+
+// Both steps by one workgroup, a wave to a sequence: fewer launches, where
+// there are few table entries to look at.
+__global__ __launch_bounds__(kThreads) void fork_or_free_few(pc_pages p, const int32_t *seq, const int32_t *child,
+                                                             int32_t n, int32_t *status) {
+    extern __shared__ uint32_t seen[];
+    __shared__ int any_bad;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (stopped(status)) return;
+    if (threadIdx.x == 0) any_bad = 0;
+    bool bad = bad_lists(p, seq, child, n, seen);
+    for (int i = wave; i < n; i += kThreads / 64) bad |= bad_pages(p, (uint32_t)seq[i], lane, 64);
+    if (bad) any_bad = 1;
+    __syncthreads();
+    if (any_bad) {
+        if (threadIdx.x == 0) *status = PC_EINVAL;
+        return;
+    }
+    for (int i = wave; i < n; i += kThreads / 64) {
+        if (child) {
+            fork_one(p, seq[i], child[i], lane, 64);
+        } else {
+            const int len = p.d_len[seq[i]];
+            free_one(p, seq[i], len, lane, 64);
+            if (lane == 0) p.d_len[seq[i]] = 0;
+        }
+    }
 }
 
 // ------------------------------------------------------------------ free pages
@@ -162,6 +205,51 @@ __global__ __launch_bounds__(256) void scan_refs(pc_pages p, PagesWs ws, const i
     if (threadIdx.x == 0) ws.chunk_free[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
 }
 
+// A pool of so many pages or fewer is scanned by the one workgroup that plans,
+// in place of two kernels of their own: 2 us less than their launches take at
+// 512 pages, even at 16,384.
+constexpr int kSmallPool = 16384;
+
+// Free pages as bits, with those before each word.
+struct FreeBits {
+    uint64_t bits[kSmallPool / 64];
+    int32_t before[kSmallPool / 64];
+    __device__ bool is_free(int page) const { return bits[page >> 6] >> (page & 63) & 1; }
+    // free pages before this one
+    __device__ int rank(int page) const {
+        return before[page >> 6] + __popcll(bits[page >> 6] & ((1ull << (page & 63)) - 1));
+    }
+};
+
+// Scans a small pool by one workgroup; all its free pages.
+__device__ int scan_small(const pc_pages &p, FreeBits &f, int *lds) {
+    const int lane = threadIdx.x & 63, words = (p.n_pages + 63) / 64;
+    for (int w = threadIdx.x >> 6; w < words; w += kThreads / 64) {
+        const int page = w * 64 + lane;
+        const uint64_t m = __ballot(page < p.n_pages && p.d_refs[page] == 0);
+        if (lane == 0) f.bits[w] = m;
+    }
+    __syncthreads();
+    int all;
+    const int t = threadIdx.x, x = block_sum<kThreads>(t < words ? (int)__popcll(f.bits[t]) : 0, &all, lds);
+    if (t < words) f.before[t] = x;
+    __syncthreads();
+    return all;
+}
+
+// One chunk of a scanned pool, by 256 threads.
+__device__ void load_chunk(const PagesWs &ws, FreeBits &f, int *lds) {
+    const int t = threadIdx.x;
+    const uint64_t m = t < 64 ? ws.free_bits[(int64_t)blockIdx.x * 64 + t] : 0;
+    int all;
+    const int x = ws.chunk_free[blockIdx.x] + block_sum<256>((int)__popcll(m), &all, lds);
+    if (t < 64) {
+        f.bits[t] = m;
+        f.before[t] = x;
+    }
+    __syncthreads();
+}
+
 // Free pages of all chunks; chunk_free becomes those before the chunk.  One
 // workgroup, all of its threads.
 __device__ int sum_chunks(const PagesWs &ws, int *lds) {
@@ -170,7 +258,7 @@ __device__ int sum_chunks(const PagesWs &ws, int *lds) {
         const int c = c0 + threadIdx.x;
         const int v = c < ws.n_chunks ? ws.chunk_free[c] : 0;
         int all;
-        const int x = block_sum(v, &all, lds);
+        const int x = block_sum<kThreads>(v, &all, lds);
         if (c < ws.n_chunks) ws.chunk_free[c] = before + x;
         before += all;
     }
@@ -183,45 +271,59 @@ __device__ int sum_chunks(const PagesWs &ws, int *lds) {
 // every sequence its ranks among the free pages, and takes the copied pages'
 // holders off them.  A shared last page's count tells whether all its holders
 // grow: each takes itself off, and where nothing is left the lowest place in
-// the list, found by an atomic minimum in the same word, keeps the page.
+// the list, found by an atomic minimum in the same word, keeps the page.  (A
+// barrier waits for a wave's atomics, and the loads that follow go past L1, so
+// no fence is needed within the workgroup.)
+template <bool kSmall>
 __global__ __launch_bounds__(kThreads) void extend_plan(pc_pages p, const int32_t *seq, const int32_t *add, int32_t n,
                                                         PagesWs ws, int32_t *status) {
     if (*status != PC_OK) return;
+    constexpr int kPer = PC_MAX_BATCH / kThreads;
     extern __shared__ uint32_t seen[];
+    __shared__ FreeBits free_bits;
     __shared__ int lds[16];
     __shared__ int64_t lds64[16];
-    __shared__ int any_bad;
+    __shared__ int any_bad, any_shared;
     int32_t *first = ws.entry, *have = first + n, *fresh = have + n, *copied = fresh + n;
     const int words = (p.n_seqs + 31) / 32;
     for (int i = threadIdx.x; i < words; i += kThreads) seen[i] = 0;
-    if (threadIdx.x == 0) {
-        any_bad = 0;
-        ws.head[0] = 0;
-    }
+    if (threadIdx.x == 0) any_bad = any_shared = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kThreads) {
+    auto count = [&](int page) {
+        return __hip_atomic_load(&p.d_refs[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    };
+    int need[kPer], last[kPer];     // new pages; a shared last page, or -1
+    bool keeps[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int i = e * kThreads + threadIdx.x;
+        need[e] = 0;
+        last[e] = -1;
+        keeps[e] = false;
+        if (i >= n) continue;
         const uint32_t s = (uint32_t)seq[i];
         const int a = add[i];
         bool bad = s >= (uint32_t)p.n_seqs || a < 0;
-        int src = -1, nb = 0, more = 0;
         if (!bad) {
             const uint32_t bit = 1u << (s & 31);
             const int len = p.d_len[s];
             bad = (atomicOr(&seen[s >> 5], bit) & bit) || !len_ok(p, len) ||
                   (int64_t)len + a > (int64_t)p.table_width * kBlk;
             if (!bad) {
-                nb = blocks_of(len);
-                more = blocks_of(len + a) - nb;
+                const int nb = blocks_of(len);
+                need[e] = blocks_of(len + a) - nb;
+                have[i] = nb;
                 if (a > 0 && len % kBlk) {
                     const int page = p.d_table[(int64_t)s * p.table_width + nb - 1];
-                    if (!page_ok(p, page)) bad = true;
-                    else if (p.d_refs[page] > 1) src = page;
+                    if (!page_ok(p, page)) {
+                        bad = true;
+                    } else if (count(page) > 1) {
+                        last[e] = page;
+                        any_shared = 1;
+                    }
                 }
             }
         }
-        have[i] = nb;
-        fresh[i] = more;
-        copied[i] = src;
         if (bad) any_bad = 1;
     }
     __syncthreads();
@@ -229,72 +331,85 @@ __global__ __launch_bounds__(kThreads) void extend_plan(pc_pages p, const int32_
         if (threadIdx.x == 0) *status = PC_EINVAL;
         return;
     }
-    for (int i = threadIdx.x; i < n; i += kThreads)
-        if (copied[i] >= 0) atomicSub(&p.d_refs[copied[i]], 1);
-    __threadfence();
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kThreads)
-        if (copied[i] >= 0 &&
-            __hip_atomic_load(&p.d_refs[copied[i]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) <= 0)
-            atomicMin(&p.d_refs[copied[i]], i - n);
-    __threadfence();
-    __syncthreads();
-    int64_t total = 0;
-    for (int i0 = 0; i0 < n; i0 += kThreads) {
-        const int i = i0 + threadIdx.x;
-        int need = 0;
-        if (i < n) {
-            need = fresh[i];
-            if (copied[i] >= 0) {
-                const int at = __hip_atomic_load(&p.d_refs[copied[i]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                if (at == i - n) copied[i] = -2 - copied[i];    // keeps it
-                else ++need;
+    const int n_free = kSmall ? scan_small(p, free_bits, lds) : sum_chunks(ws, lds);
+    if (any_shared) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (last[e] >= 0) atomicSub(&p.d_refs[last[e]], 1);
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (last[e] >= 0 && count(last[e]) <= 0) atomicMin(&p.d_refs[last[e]], e * kThreads + (int)threadIdx.x - n);
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (last[e] >= 0) {
+                keeps[e] = count(last[e]) == e * kThreads + (int)threadIdx.x - n;
+                if (!keeps[e]) ++need[e];
             }
-        }
+    }
+    int64_t total = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        if (e * kThreads >= n) break;
+        const int i = e * kThreads + threadIdx.x;
         int64_t all;
-        const int64_t x = block_sum((int64_t)need, &all, lds64);
+        const int64_t x = block_sum<kThreads>((int64_t)need[e], &all, lds64);
         if (i < n) {
             first[i] = (int32_t)(total + x);    // of use only where the pool has them all
-            fresh[i] = need;
+            fresh[i] = need[e];
+            copied[i] = keeps[e] ? -1 : last[e];
         }
         total += all;
     }
-    const bool short_of = total > sum_chunks(ws, lds);
-    __syncthreads();
-    // the counts: kept pages have one holder again; where the pool is short, all as before
-    for (int i = threadIdx.x; i < n; i += kThreads)
-        if (copied[i] <= -2)
-            __hip_atomic_store(&p.d_refs[-2 - copied[i]], short_of ? 0 : 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __threadfence();
-    __syncthreads();
+    const bool short_of = total > n_free;
+    if (any_shared) {
+        // kept pages have one holder again; where the pool is short, all is as before
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (keeps[e])
+                __hip_atomic_store(&p.d_refs[last[e]], short_of ? 0 : 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (short_of)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (last[e] >= 0) atomicAdd(&p.d_refs[last[e]], 1);
+    }
     if (short_of) {
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            if (copied[i] == -1) continue;
-            atomicAdd(&p.d_refs[copied[i] <= -2 ? -2 - copied[i] : copied[i]], 1);
-        }
         if (threadIdx.x == 0) *status = PC_ENOPAGES;
-    } else if (threadIdx.x == 0) {
-        ws.head[0] = (int32_t)total;
+        return;
+    }
+    if (!kSmall) {
+        if (threadIdx.x == 0) ws.head[0] = (int32_t)total;
+    } else if (total) {
+        for (int page = threadIdx.x; page < p.n_pages; page += kThreads)
+            if (free_bits.is_free(page)) {
+                const int rank = free_bits.rank(page);
+                if (rank < total) {
+                    ws.list[rank] = page;
+                    p.d_refs[page] = 1;
+                }
+            }
     }
 }
 
 // The free pages of rank < head[0], listed by rank; they have a holder now.
 __global__ __launch_bounds__(256) void list_free(pc_pages p, PagesWs ws, const int32_t *status) {
     if (*status != PC_OK) return;
+    __shared__ FreeBits f;
     __shared__ int lds[4];
-    const int total = ws.head[0];
-    const int before = ws.chunk_free[blockIdx.x];
-    if (before >= total) return;
-    const int t = threadIdx.x;
-    const uint64_t m = t < 64 ? ws.free_bits[(int64_t)blockIdx.x * 64 + t] : 0;
-    int all;
-    int rank = before + block_sum((int)__popcll(m), &all, lds);
-    const int base = blockIdx.x * kChunkPages + t * 64;
-    for (uint64_t x = m; x && rank < total; x &= x - 1, ++rank) {
-        const int page = base + __ffsll((unsigned long long)x) - 1;
-        ws.list[rank] = page;
-        p.d_refs[page] = 1;
-    }
+    const int total = ws.head[0], base = blockIdx.x * kChunkPages;
+    if (ws.chunk_free[blockIdx.x] >= total) return;
+    load_chunk(ws, f, lds);
+    for (int at = threadIdx.x; at < kChunkPages; at += 256)
+        if (f.is_free(at)) {        // no page behind the pool's last is
+            const int rank = f.rank(at);
+            if (rank < total) {
+                ws.list[rank] = base + at;
+                p.d_refs[base + at] = 1;
+            }
+        }
 }
 
 __global__ __launch_bounds__(256) void extend_pages(pc_pages p, const int32_t *seq, const int32_t *add, int32_t n,
@@ -313,17 +428,33 @@ __global__ __launch_bounds__(256) void extend_pages(pc_pages p, const int32_t *s
 
 // ------------------------------------------------------------------ compact
 
+// A page's part in the moves: the free places before n_live and the pages
+// behind it are listed by rank.  free_before: free pages before this one.
+__device__ __forceinline__ void list_move(const PagesWs &ws, int page, bool is_free, int free_before, int live, int holes) {
+    if (is_free) {
+        if (page < live) ws.list[free_before] = page;
+    } else if (page >= live) {
+        const int i = page - free_before - (live - holes);      // pages in use before it, less those that stay
+        ws.moved[i] = page;
+        ws.rank[page] = i;
+    }
+}
+
 // One workgroup: pages in use, and how many of them lie behind that number.
+template <bool kSmall>
 __global__ __launch_bounds__(kThreads) void compact_plan(pc_pages p, PagesWs ws, int32_t *n_live, const int32_t *status) {
     if (*status != PC_OK) {
         if (threadIdx.x == 0) ws.head[3] = 0;
         return;
     }
+    __shared__ FreeBits free_bits;
     __shared__ int lds[16];
-    const int live = p.n_pages - sum_chunks(ws, lds);
+    const int live = p.n_pages - (kSmall ? scan_small(p, free_bits, lds) : sum_chunks(ws, lds));
     __syncthreads();
     int holes = 0;
-    if (live < p.n_pages) {
+    if (live < p.n_pages && kSmall) {
+        holes = free_bits.rank(live);
+    } else if (live < p.n_pages) {
         // free pages before page `live`
         const int c = live / kChunkPages, in = live % kChunkPages, t = threadIdx.x;
         int x = 0;
@@ -333,8 +464,13 @@ __global__ __launch_bounds__(kThreads) void compact_plan(pc_pages p, PagesWs ws,
             x = __popcll(bits >= 64 ? m : m & ((1ull << bits) - 1));
         }
         int all;
-        block_sum(x, &all, lds);
+        block_sum<kThreads>(x, &all, lds);
         holes = ws.chunk_free[c] + all;
+    }
+    if (kSmall) {
+        for (int page = threadIdx.x; page < p.n_pages; page += kThreads)
+            list_move(ws, page, free_bits.is_free(page), free_bits.rank(page), live, holes);
+        for (int w = threadIdx.x; w < (p.n_pages + 63) / 64; w += kThreads) ws.free_bits[w] = free_bits.bits[w];
     }
     if (threadIdx.x == 0) {
         ws.head[0] = live;
@@ -344,32 +480,14 @@ __global__ __launch_bounds__(kThreads) void compact_plan(pc_pages p, PagesWs ws,
     }
 }
 
-// Rank by rank: the free places before n_live, and the pages behind it.
 __global__ __launch_bounds__(256) void list_moves(pc_pages p, PagesWs ws, const int32_t *status) {
     if (*status != PC_OK) return;
+    __shared__ FreeBits f;
     __shared__ int lds[4];
-    const int live = ws.head[0], holes = ws.head[1], t = threadIdx.x;
-    const uint64_t m = t < 64 ? ws.free_bits[(int64_t)blockIdx.x * 64 + t] : 0;
-    const int base = blockIdx.x * kChunkPages + t * 64;
-    int all;
-    const int free_before = ws.chunk_free[blockIdx.x] + block_sum((int)__popcll(m), &all, lds);
-    if (t >= 64 || base >= p.n_pages) return;
-    int rank = free_before;
-    for (uint64_t x = m; x && rank < holes; x &= x - 1, ++rank)
-        ws.list[rank] = base + __ffsll((unsigned long long)x) - 1;
-    const int bits = p.n_pages - base;
-    uint64_t used = ~m;
-    if (bits < 64) used &= (1ull << bits) - 1;
-    // pages in use before this word, less those that stay
-    int moves = base - free_before - (live - holes);
-    for (; used; used &= used - 1) {
-        const int page = base + __ffsll((unsigned long long)used) - 1;
-        if (page >= live) {
-            ws.moved[moves] = page;
-            ws.rank[page] = moves;
-        }
-        ++moves;
-    }
+    const int live = ws.head[0], holes = ws.head[1], base = blockIdx.x * kChunkPages;
+    load_chunk(ws, f, lds);
+    for (int at = threadIdx.x; at < kChunkPages && base + at < p.n_pages; at += 256)
+        list_move(ws, base + at, f.is_free(at), f.rank(at), live, holes);
 }
 
 __global__ __launch_bounds__(256) void compact_pages(pc_pages p, int32_t *refs_to, int32_t *table_to, PagesWs ws,
@@ -541,7 +659,7 @@ __global__ __launch_bounds__(kThreads) void group_requests(const uint64_t *keys,
         const int l = x / PC_MAX_BATCH, i = x % PC_MAX_BATCH;
         const bool begins = q < R && (q == 0 || lead[q - 1] / PC_MAX_BATCH != l);
         int all;
-        const int g = groups + block_sum((int)begins, &all, lds) + begins - 1;
+        const int g = groups + block_sum<kThreads>((int)begins, &all, lds) + begins - 1;
         if (q < R) order[q] = g * PC_MAX_BATCH + i;
         if (begins) {
             const bool alone = q + 1 >= R || lead[q + 1] / PC_MAX_BATCH != l;
@@ -614,33 +732,53 @@ int64_t pages_ws(const pc_pages &p, int64_t n, char *base, PagesWs *ws) {
 
 static size_t seen_bytes(const pc_pages &p) { return (size_t)((p.n_seqs + 31) / 32) * 4; }
 
+// Table entries up to which one workgroup forks or frees by itself: 2 us less
+// than two launches for a few sequences, as long at 8,192 entries.
+constexpr int64_t kFewEntries = 8192;
+
 hipError_t launch_fork(const pc_pages &p, const int32_t *parent, const int32_t *child, int32_t n, int32_t *status,
                        hipStream_t st) {
-    check_lists<<<n + 1, kThreads, seen_bytes(p), st>>>(p, parent, child, n, status);
-    fork_pages<<<n, 256, 0, st>>>(p, parent, child, status);
+    if ((int64_t)n * p.table_width <= kFewEntries) {
+        fork_or_free_few<<<1, kThreads, seen_bytes(p), st>>>(p, parent, child, n, status);
+    } else {
+        check_lists<<<n + 1, 256, seen_bytes(p), st>>>(p, parent, child, n, status);
+        fork_pages<<<n, 256, 0, st>>>(p, parent, child, status);
+    }
     return hipGetLastError();
 }
 
 hipError_t launch_free(const pc_pages &p, const int32_t *seq, int32_t n, int32_t *status, hipStream_t st) {
-    check_lists<<<n + 1, kThreads, seen_bytes(p), st>>>(p, seq, nullptr, n, status);
-    free_pages<<<n, 256, 0, st>>>(p, seq, status);
+    if ((int64_t)n * p.table_width <= kFewEntries) {
+        fork_or_free_few<<<1, kThreads, seen_bytes(p), st>>>(p, seq, nullptr, n, status);
+    } else {
+        check_lists<<<n + 1, 256, seen_bytes(p), st>>>(p, seq, nullptr, n, status);
+        free_pages<<<n, 256, 0, st>>>(p, seq, status);
+    }
     return hipGetLastError();
 }
 
 hipError_t launch_extend(const pc_pages &p, const int32_t *seq, const int32_t *add, int32_t n, const PagesWs &ws,
                          int32_t *status, hipStream_t st) {
-    scan_refs<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
-    extend_plan<<<1, kThreads, seen_bytes(p), st>>>(p, seq, add, n, ws, status);
-    list_free<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+    if (p.n_pages <= kSmallPool) {
+        extend_plan<true><<<1, kThreads, seen_bytes(p), st>>>(p, seq, add, n, ws, status);
+    } else {
+        scan_refs<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+        extend_plan<false><<<1, kThreads, seen_bytes(p), st>>>(p, seq, add, n, ws, status);
+        list_free<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+    }
     extend_pages<<<dim3(n, 2 * p.n_layers), 256, 0, st>>>(p, seq, add, n, ws, status);
     return hipGetLastError();
 }
 
 hipError_t launch_compact(const pc_pages &p, int32_t *refs_to, int32_t *table_to, int32_t *n_live, const PagesWs &ws,
                           int32_t *status, hipStream_t st) {
-    scan_refs<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
-    compact_plan<<<1, kThreads, 0, st>>>(p, ws, n_live, status);
-    list_moves<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+    if (p.n_pages <= kSmallPool) {
+        compact_plan<true><<<1, kThreads, 0, st>>>(p, ws, n_live, status);
+    } else {
+        scan_refs<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+        compact_plan<false><<<1, kThreads, 0, st>>>(p, ws, n_live, status);
+        list_moves<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+    }
     compact_pages<<<2048, 256, 0, st>>>(p, refs_to, table_to, ws, status);
     return hipGetLastError();
 }

@@ -101,6 +101,7 @@ int32_t pc_pages_extend(const pc_pages *pages, const int32_t *d_seq, const int32
                         void *d_workspace, int64_t workspace_bytes, int32_t *d_status, void *stream) {
     if (int32_t rc = check_pool(pages)) return rc;
     if (int32_t rc = check_list(pages, n, d_seq, d_add, d_status)) return rc;
+    if (n > PC_MAX_BATCH) return fail(PC_EUNSUPPORTED, "%d sequences: at most %d", n, PC_MAX_BATCH);
     if (int32_t rc = check_ws(d_workspace, workspace_bytes, pages_ws(*pages, n, nullptr, nullptr))) return rc;
     if (n == 0) return ok();
     PagesWs ws;

@@ -267,8 +267,8 @@ def _need(ok, message):
 
 
 def _list(x, dev, what, dtype=torch.int32):
-    _need(x.dtype == dtype and x.device == dev and x.dim() == 1 and x.is_contiguous(),
-          f"{what}: a contiguous one-dimensional {dtype} tensor on {dev}")
+    if not (x.dtype is dtype and x.get_device() == dev.index and x.dim() == 1 and x.is_contiguous()):
+        raise ValueError(f"{what}: a contiguous one-dimensional {dtype} tensor on {dev}")
     return x
 
 
@@ -378,10 +378,11 @@ class PagePool:
                            k_new.shape[0], make_rows(k_new), make_rows(v_new), self.status, stream)
 
     def _rows(self, x, heads, what):
-        d = self.desc
-        _need(x.dim() == 3 and x.shape[1] == heads and x.shape[2] == d.head_dim and x.dtype == self.k.dtype
-              and x.device == self.device and (x.stride(2) == 1 or x.numel() == 0),
-              f"{what}: [tokens, {heads}, {d.head_dim}] of {self.k.dtype} on {self.device}, the last dimension contiguous")
+        dim = self.desc.head_dim
+        if not (x.dim() == 3 and x.shape[1] == heads and x.shape[2] == dim and x.dtype is self.k.dtype
+                and x.get_device() == self.device.index and x.stride(2) == 1):
+            raise ValueError(f"{what}: [tokens, {heads}, {dim}] of {self.k.dtype} on {self.device}, "
+                             "the last dimension contiguous")
 
 
 class PrefixGroups(NamedTuple):
@@ -425,13 +426,13 @@ class PrefixBatch:
         q_off[r+1]-1, its last tokens; order .. n_groups: its groups, as
         prefix_groups gives them, or none."""
         pool, R = self.pool, self.n_req
-        _need(seq.numel() == R and q_off.numel() == R + 1, f"seq and q_off of {R} requests")
+        _need(seq.numel() == R and q_off.numel() == R + 1, "seq: one for each request, q_off: one more")
         given = [x for x in (order, group_off, shared, n_groups) if x is not None]
-        _need(len(given) in (0, 4), "groups: all of order, group_off, shared and n_groups, or none")
         if given:
-            _need([x.numel() for x in given] == [R, R + 1, R, 1], f"groups of {R} requests")
-        for x in given:
-            _list(x, pool.device, "groups")
+            _need(len(given) == 4, "groups: all of order, group_off, shared and n_groups, or none")
+            _need([x.numel() for x in given] == [R, R + 1, R, 1], "groups of as many requests")
+            for x in given:
+                _list(x, pool.device, "groups")
         with _on(pool.device, stream):
             pc_attn_plan(pool.desc, _list(seq, pool.device, "seq"), _list(q_off, pool.device, "q_off"), self.n_tokens,
                          self.n_heads, causal, order, group_off, shared, n_groups, self.workspace, pool.status, stream)
@@ -446,7 +447,7 @@ class PrefixBatch:
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
             for x in (q, out):
                 pool._rows(x, self.n_heads, "q and out")
-                _need(x.shape[0] == self.n_tokens, f"q and out: {self.n_tokens} tokens")
+                _need(x.shape[0] == self.n_tokens, "q and out: as many tokens as the batch has")
             _need(lse is None or (lse.shape == q.shape[:2] and lse.dtype == torch.float32 and lse.is_contiguous()
                                   and lse.device == pool.device), "lse: a contiguous float32 [tokens, heads]")
             if scale is None:

@@ -104,6 +104,7 @@ def test_what_is_not_implemented():
     assert _plan(_pool(), n=P.PC_MAX_BATCH + 1, tokens=P.PC_MAX_BATCH + 1) == P.PC_EUNSUPPORTED
     assert _plan(_pool(), tokens=1 << 28, heads=64) == P.PC_EUNSUPPORTED     # over 2^31 partial rows
     assert _groups(n=P.PC_MAX_BATCH + 1) == P.PC_EUNSUPPORTED
+    assert _extend(_pool(n_seqs=P.PC_MAX_BATCH + 1), n=P.PC_MAX_BATCH + 1) == P.PC_EUNSUPPORTED
 
 
 @pytest.mark.parametrize("kw", [dict(n=0), dict(w=0), dict(n_keys=-1), dict(keys=None), dict(keys=FAKE + 4),
