@@ -549,77 +549,86 @@ __global__ __launch_bounds__(256) void write_rows(pc_pages p, int32_t layer, con
     } else {
         const int32_t *row = p.d_table + (int64_t)s * p.table_width;
         const int per_row = p.head_dim / 8, units = p.n_kv_heads * per_row;
-        const int64_t layer_off = (int64_t)layer * p.layer_stride;
         const int32_t head_stride = p.layout == PC_HEADS_FIRST ? kBlk * p.head_dim : p.head_dim;
         const int32_t token_stride = p.layout == PC_HEADS_FIRST ? p.head_dim : p.n_kv_heads * p.head_dim;
-        const int64_t all = (r1 - r0) * units;
-        for (int64_t u = (int64_t)blockIdx.y * blockDim.x + threadIdx.x; u < all; u += (int64_t)gridDim.y * blockDim.x) {
-            const int64_t j = u / units;
-            const int w = (int)(u - j * units), h = w / per_row, c = w - h * per_row;
-            const int pos = (int)(len - (r1 - r0) + j);
-            const int page = row[pos / kBlk];
-            if (!page_ok(p, page) || p.d_refs[page] != 1) {
-                bad = true;
-                continue;
+        uint16_t *kp = static_cast<uint16_t *>(p.d_k) + (int64_t)layer * p.layer_stride;
+        uint16_t *vp = static_cast<uint16_t *>(p.d_v) + (int64_t)layer * p.layer_stride;
+        // as many tokens at a time as a workgroup's threads have pieces for
+        const int tokens = units < 256 ? 256 / units : 1, n_new = (int)(r1 - r0);
+        const int my_token = (int)threadIdx.x / units, w0 = (int)threadIdx.x - my_token * units;
+        for (int j = blockIdx.y * tokens + my_token; my_token < tokens && j < n_new; j += gridDim.y * tokens)
+            for (int w = w0; w < units; w += 256) {
+                const int h = w / per_row, c = w - h * per_row;
+                const uint4 k = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(kn.d_data) +
+                                                                 (r0 + j) * kn.token_stride + h * kn.head_stride + c * 8);
+                const uint4 v = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(vn.d_data) +
+                                                                 (r0 + j) * vn.token_stride + h * vn.head_stride + c * 8);
+                const int pos = len - n_new + j, page = row[pos / kBlk];
+                if (!page_ok(p, page) || p.d_refs[page] != 1) {
+                    bad = true;
+                    continue;
+                }
+                const int64_t to = page * p.page_stride + (pos % kBlk) * token_stride + h * head_stride + c * 8;
+                *reinterpret_cast<uint4 *>(kp + to) = k;
+                *reinterpret_cast<uint4 *>(vp + to) = v;
             }
-            const int64_t to = layer_off + page * p.page_stride + (pos % kBlk) * token_stride + h * head_stride + c * 8;
-            const int64_t kf = (r0 + j) * kn.token_stride + h * kn.head_stride + c * 8;
-            const int64_t vf = (r0 + j) * vn.token_stride + h * vn.head_stride + c * 8;
-            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.d_k) + to) =
-                *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(kn.d_data) + kf);
-            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.d_v) + to) =
-                *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(vn.d_data) + vf);
-        }
     }
     if (bad) atomicExch(status, PC_EINVAL);
 }
 
 // ------------------------------------------------------------------ groups
 
-// One workgroup: the first request with the same key of block min_blocks - 1
-// by a hash table in LDS, then a sort by (that request, own number).  Leaves
-// each request's group beside its number in d_order for the next kernel, and
-// the first request's blocks in d_shared.
-__global__ __launch_bounds__(kThreads) void group_requests(const uint64_t *keys, int64_t n_keys, const int64_t *key_off,
-                                                           int32_t R, int32_t Rp, int32_t min_blocks, int32_t *order,
-                                                           int32_t *group_off, int32_t *shared, int32_t *n_groups,
-                                                           int32_t *status) {
+// One workgroup of NT threads, for up to NT * kPer requests: the first request
+// with the same key of block min_blocks - 1 by a hash table in LDS, then a sort
+// by (that request, own number): a bitonic network whose exchanges within a
+// wave go by registers, so that 10 of the 55 steps for 1,024 requests need a
+// barrier (21 us before, with one at every step).  Leaves each request's group
+// beside its number in d_order for the next kernel, and the first request's
+// blocks in d_shared.
+template <int NT, int kPer>
+__global__ __launch_bounds__(NT) void group_requests(const uint64_t *keys, int64_t n_keys, const int64_t *key_off,
+                                                     int32_t R, int32_t Rp, int32_t min_blocks, int32_t *order,
+                                                     int32_t *group_off, int32_t *shared, int32_t *n_groups,
+                                                     int32_t *status) {
     if (*status != PC_OK) return;
     extern __shared__ __align__(16) uint64_t mark[];          // [Rp]
     int32_t *lead = reinterpret_cast<int32_t *>(mark + Rp);   // [Rp] then the sorted words
     int32_t *tab = lead + Rp;                                 // [2 Rp]
-    __shared__ int lds[16];
+    __shared__ int lds[NT / 64];
     __shared__ int any_bad;
-    if (threadIdx.x == 0) any_bad = 0;
-    for (int i = threadIdx.x; i < 2 * Rp; i += kThreads) tab[i] = -1;
+    const int tid = threadIdx.x;
+    if (tid == 0) any_bad = 0;
+    for (int i = tid; i < 2 * Rp; i += NT) tab[i] = -1;
     __syncthreads();
-    for (int i = threadIdx.x; i < Rp; i += kThreads) {
-        lead[i] = i;
-        if (i < R) {
-            const int64_t a = key_off[i], b = key_off[i + 1];
-            if (a < 0 || b < a || b > n_keys || b - a > (1 << 26)) any_bad = 1;
-            else if (b - a >= min_blocks) mark[i] = keys[a + min_blocks - 1];
-        }
+    int blocks[kPer], word[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int i = e * NT + tid;
+        blocks[e] = 0;
+        if (i < Rp) lead[i] = i;
+        if (i >= R) continue;
+        const int64_t a = key_off[i], b = key_off[i + 1];
+        if (a < 0 || b < a || b > n_keys || b - a > 1 << 26) any_bad = 1;
+        else blocks[e] = (int)(b - a);
+        if (blocks[e] >= min_blocks) mark[i] = keys[a + min_blocks - 1];
     }
     __syncthreads();
     if (any_bad) {
-        if (threadIdx.x == 0) *status = PC_EINVAL;
+        if (tid == 0) *status = PC_EINVAL;
         return;
     }
-    constexpr int kPer = PC_MAX_BATCH / kThreads;
-    int rep[kPer];
     const uint32_t slots = 2 * Rp;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
-        const int i = e * kThreads + threadIdx.x;
-        rep[e] = i;
-        if (i >= R || key_off[i + 1] - key_off[i] < min_blocks) continue;
+        const int i = e * NT + tid;
+        word[e] = i;        // a request that has this one's key
+        if (i >= R || blocks[e] < min_blocks) continue;
         uint32_t at = (uint32_t)((mark[i] * 0x9E3779B97F4A7C15ull) >> 40) & (slots - 1);
-        for (;;) {      // at most half of the slots are ever taken
+        for (;;) {          // at most half of the slots are ever taken
             const int cur = atomicCAS(&tab[at], -1, i);
             if (cur < 0) break;
             if (mark[cur] == mark[i]) {
-                rep[e] = cur;
+                word[e] = cur;
                 atomicMin(&lead[cur], i);
                 break;
             }
@@ -627,39 +636,58 @@ __global__ __launch_bounds__(kThreads) void group_requests(const uint64_t *keys,
         }
     }
     __syncthreads();
-    int word[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
-        const int i = e * kThreads + threadIdx.x;
-        word[e] = i < R ? lead[rep[e]] * PC_MAX_BATCH + i : 0x7fffffff;
+        const int i = e * NT + tid;
+        word[e] = i < R ? lead[word[e]] * PC_MAX_BATCH + i : 0x7fffffff;
     }
     __syncthreads();
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const int i = e * kThreads + threadIdx.x;
-        if (i < Rp) lead[i] = word[e];
-    }
-    __syncthreads();
+    int32_t *to = lead, *other = tab;       // exchanged in turn: one barrier a step
     for (int k = 2; k <= Rp; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int t = threadIdx.x; t < Rp / 2; t += kThreads) {
-                const int a = (t / j) * 2 * j + t % j, b = a + j;
-                const int x = lead[a], y = lead[b];
-                if ((x > y) == ((a & k) == 0)) {
-                    lead[a] = y;
-                    lead[b] = x;
+            int theirs[kPer];
+            if (j >= NT) {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    theirs[e] = 0;
+#pragma unroll
+                    for (int x = 0; x < kPer; ++x)
+                        if (x == (e ^ (j / NT))) theirs[e] = word[x];
                 }
+            } else if (j >= 64) {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if (e * NT + tid < Rp) to[e * NT + tid] = word[e];
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) theirs[e] = e * NT + tid < Rp ? to[(e * NT + tid) ^ j] : 0;
+                int32_t *t = to;
+                to = other;
+                other = t;
+            } else {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) theirs[e] = __shfl_xor(word[e], j);
             }
-            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const int i = e * NT + tid;
+                const bool least = ((i & j) == 0) == ((i & k) == 0);
+                word[e] = least ? min(word[e], theirs[e]) : max(word[e], theirs[e]);
+            }
         }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+        if (e * NT + tid < Rp) lead[e * NT + tid] = word[e];
+    __syncthreads();
     int groups = 0;
-    for (int p0 = 0; p0 < R; p0 += kThreads) {
-        const int q = p0 + threadIdx.x;
+    for (int p0 = 0; p0 < R; p0 += NT) {
+        const int q = p0 + tid;
         const int x = q < R ? lead[q] : 0;
         const int l = x / PC_MAX_BATCH, i = x % PC_MAX_BATCH;
         const bool begins = q < R && (q == 0 || lead[q - 1] / PC_MAX_BATCH != l);
         int all;
-        const int g = groups + block_sum<kThreads>((int)begins, &all, lds) + begins - 1;
+        const int g = groups + block_sum<NT>((int)begins, &all, lds) + begins - 1;
         if (q < R) order[q] = g * PC_MAX_BATCH + i;
         if (begins) {
             const bool alone = q + 1 >= R || lead[q + 1] / PC_MAX_BATCH != l;
@@ -668,11 +696,11 @@ __global__ __launch_bounds__(kThreads) void group_requests(const uint64_t *keys,
         }
         groups += all;
     }
-    for (int g = groups + threadIdx.x; g <= R; g += kThreads) {
+    for (int g = groups + tid; g <= R; g += NT) {
         group_off[g] = R;
         if (g < R) shared[g] = 0;
     }
-    if (threadIdx.x == 0) *n_groups = groups;
+    if (tid == 0) *n_groups = groups;
 }
 
 // A workgroup for each request: how many leading keys it has in common with
@@ -785,9 +813,10 @@ hipError_t launch_compact(const pc_pages &p, int32_t *refs_to, int32_t *table_to
 
 hipError_t launch_write(const pc_pages &p, int32_t layer, const int32_t *seq, const int32_t *new_off, int32_t n,
                         int64_t n_tokens, const pc_rows &k_new, const pc_rows &v_new, int32_t *status, hipStream_t st) {
-    // workgroups enough for the case that one sequence has all the tokens, but not over 4096 in all
-    int64_t y = (n_tokens * p.n_kv_heads * (p.head_dim / 8) + 1023) / 1024;
-    const int64_t most = 4096 / n > 1 ? 4096 / n : 1;
+    // workgroups enough for the case that one sequence has all the tokens, but not many more than the chip
+    // holds at a time
+    int64_t y = (n_tokens * p.n_kv_heads * (p.head_dim / 8) + 255) / 256;
+    const int64_t most = 8192 / n > 1 ? 8192 / n : 1;
     y = y < 1 ? 1 : y > most ? most : y;
     write_rows<<<dim3(n + 1, (uint32_t)y), 256, seen_bytes(p), st>>>(p, layer, seq, new_off, n, n_tokens, k_new, v_new, status);
     return hipGetLastError();
@@ -799,13 +828,22 @@ hipError_t launch_groups(const uint64_t *keys, int64_t n_keys, const int64_t *ke
     int32_t rp = 2;
     while (rp < n_req) rp <<= 1;
     const size_t bytes = (size_t)rp * (8 + 4 + 8);
-    if (bytes > 64 * 1024 - 256) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&group_requests),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        if (e != hipSuccess) return e;
-    }
-    group_requests<<<1, kThreads, bytes, st>>>(keys, n_keys, key_off, n_req, rp, min_blocks, order, group_off, shared,
-                                               n_groups, status);
+    auto launch = [&](auto *kernel, int threads) {
+        if (bytes > 64 * 1024 - 256) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+            if (e != hipSuccess) return e;
+        }
+        kernel<<<1, threads, bytes, st>>>(keys, n_keys, key_off, n_req, rp, min_blocks, order, group_off, shared,
+                                          n_groups, status);
+        return hipGetLastError();
+    };
+    // no more registers to sort than requests need (four a thread for 1,024 of them: 22 us)
+    const hipError_t e = rp <= 256    ? launch(&group_requests<256, 1>, 256)
+                         : rp <= 1024 ? launch(&group_requests<1024, 1>, 1024)
+                         : rp <= 2048 ? launch(&group_requests<1024, 2>, 1024)
+                                      : launch(&group_requests<1024, 4>, 1024);
+    if (e != hipSuccess) return e;
     group_shared<<<n_req, 256, 0, st>>>(keys, key_off, order, group_off, shared, status);
     return hipGetLastError();
 }
