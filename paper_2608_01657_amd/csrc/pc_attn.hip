@@ -368,12 +368,22 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
 
 // ------------------------------------------------------------------ wide items
 
+// Where 16-byte piece c of token t's row lies in LDS: at c ^ swap.  A row is 256
+// or 128 bytes of the banks' 256.  K is read by 16 lanes at a time, the same
+// piece of 16 tokens; V by 32 lanes of 8 bytes, which take 32 bytes each of four
+// tokens and two neighbouring columns (wide) or of eight tokens (narrow): these
+// permutations send each of them to other banks.
+template <int D>
+__device__ __forceinline__ int swap_k(int t) { return D == 128 ? t & 15 : t >> 1 & 7; }
+template <int D>
+__device__ __forceinline__ int swap_v(int t) { return D == 128 ? 4 * (t & 3) : 2 * (t & 2); }
+template <int D>
+__device__ __forceinline__ int swap_v_narrow(int t) { return D == 128 ? 2 * (t & 7) : t & 6; }
+
 // A workgroup of four waves takes 128 rows, a wave 32 of them (the columns of
 // 32 x 32 x 16 products), and 64 tokens of K and V at a time from LDS, where a
 // second pair of buffers fills meanwhile.  16-byte pieces of a token's row are
-// permuted in LDS so that neither the row reads of K nor the transposing reads
-// of V meet in a bank: piece c of token t of K is at c ^ t, of V at c ^ 2t
-// (modulo the pieces of a row).
+// permuted in LDS (see swap_k and swap_v).
 template <typename T, int D>
 __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, uint16_t *lds, int *lds_lim) {
     constexpr int kPieces = D / 8, kSteps = D / 16, kDb = D / 32, kBuf = kTileKv * D;   // K, K, V, V
@@ -419,8 +429,8 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
 #pragma unroll
     for (int i = 0; i < kPieces / 4; ++i) {
         const int u = i * 64 + lane, t = u / kPieces, c = u % kPieces;
-        k_at[i] = 2 * (t * a.token_stride + (c ^ (t & (kPieces - 1))) * 8);
-        v_at[i] = 2 * (t * a.token_stride + (c ^ (2 * t & (kPieces - 1))) * 8);
+        k_at[i] = 2 * (t * a.token_stride + (c ^ swap_k<D>(t)) * 8);
+        v_at[i] = 2 * (t * a.token_stride + (c ^ swap_v<D>(t)) * 8);
     }
     auto fetch = [&](int n, int buf, int number) {
         const uint32_t page = min((uint32_t)__builtin_amdgcn_readfirstlane(number), (uint32_t)(a.n_pages - 1));
@@ -470,7 +480,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
             for (int r = 0; r < 16; ++r) s[h][r] = 0;
 #pragma unroll
             for (int st = 0; st < kSteps; ++st) {
-                const int at = (h * 32 + col) * D + (((2 * st + half) ^ (col & (kPieces - 1))) * 8);
+                const int at = (h * 32 + col) * D + (((2 * st + half) ^ swap_k<D>(col)) * 8);
                 s[h] = T::mma32(*reinterpret_cast<const s16x8 *>(lk + at), qf[st], s[h]);
             }
         }
@@ -519,7 +529,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
         const int vt = 4 * half + quad;     // token of this lane's address, within eight
 #pragma unroll
         for (int i = 0; i < kDb; ++i) {
-            const int piece = (4 * i + 2 * g16 + ((lane & 3) >> 1)) ^ (2 * vt & (kPieces - 1));
+            const int piece = (4 * i + 2 * g16 + ((lane & 3) >> 1)) ^ swap_v<D>(vt);
             const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
 #pragma unroll
             for (int st = 0; st < 4; ++st)
@@ -620,7 +630,7 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
                 const int u = st * 64 + lane, t = u / kPieces, c = u % kPieces;
                 s16x8 v = vf[h][st];
                 if (!whole && base + h * kBlk + t >= end) v = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
-                *reinterpret_cast<s16x8 *>(lv + (h * kBlk + t) * D + (c ^ (2 * t & (kPieces - 1))) * 8) = v;
+                *reinterpret_cast<s16x8 *>(lv + (h * kBlk + t) * D + (c ^ swap_v_narrow<D>(t)) * 8) = v;
             }
         f32x4 s[kPages];
 #pragma unroll
@@ -662,7 +672,7 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
         const int vt = 4 * quarter + ((lane >> 2) & 3);     // token of this lane's address, within a page
 #pragma unroll
         for (int i = 0; i < kDb; ++i) {
-            const int piece = (2 * i + ((lane & 3) >> 1)) ^ (2 * vt & (kPieces - 1));
+            const int piece = (2 * i + ((lane & 3) >> 1)) ^ swap_v_narrow<D>(vt);
             const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
 #pragma unroll
             for (int h = 0; h < kPages; h += 2)
