@@ -427,8 +427,9 @@ int32_t pc_attn_plan(const pc_pages *pages, const int32_t *d_seq, const int32_t 
  * are the pool's table and lengths; K and V are of `layer`.  scale > 0.
  *   d_lse         optional (NULL): [n_tokens][n_heads] float, the natural
  *                 logarithm of each row's sum of exponentials
- * By a plan that set the status, nothing is written.  A page number out of
- * the pool reads another page, never memory outside. */
+ * Without a plan of these n_req, n_tokens and n_heads for this pool's shape in
+ * the workspace (also: where the plan set the status), nothing is written.  A
+ * page number out of the pool reads another page, never memory outside. */
 int32_t pc_attn(const pc_pages *pages, int32_t layer, const pc_rows *q, int32_t n_req, int64_t n_tokens,
                 int32_t n_heads, float scale, const pc_rows *out, float *d_lse, void *d_workspace,
                 int64_t workspace_bytes, void *stream);

@@ -59,16 +59,13 @@ struct Fp16 {
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -__builtin_inff();
 
-using as1 = __attribute__((address_space(1))) void;
 using as3 = __attribute__((address_space(3))) void;
 
-__device__ __forceinline__ void load_lds16(const void *g, void *l) {
-    __builtin_amdgcn_global_load_lds((const as1 *)g, (as3 *)l, 16, 0, 0);
-}
-// The same without the compiler's knowledge that LDS is written, for buffers
-// that are waited for by hand: it would wait for all loads in flight before
-// the next read of any LDS.  There is no output register to be overwritten.
-__device__ __forceinline__ void load_lds16_later(const void *g, const void *l) {
+// 16 bytes a lane from memory to LDS, at l + 16 lane, waited for by hand: the
+// compiler, told that LDS is written, would wait for all loads in flight
+// before the next read of any LDS.  There is no output register to be
+// overwritten.
+__device__ __forceinline__ void load_lds16(const void *g, const void *l) {
     const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const as3 *)l);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(g) : "memory", "m0");
 }
@@ -80,7 +77,7 @@ __device__ __forceinline__ s16x8 join(s16x4 a, s16x4 b) {
 }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
-__device__ __forceinline__ void load_lds16_later(const void *base, uint32_t offset, const void *l) {
+__device__ __forceinline__ void load_lds16(const void *base, uint32_t offset, const void *l) {
     const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const as3 *)l);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base)
                  : "memory", "m0");
@@ -363,7 +360,17 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
     if (!first) return;
     for (int j = tid; j < R; j += NT)
         ws.parts[R + j] = group(j) == kNoGroup ? AttnParts{0, 0, 0, 0} : ws.parts[2 * R + group(j)];
-    if (tid == 0) *ws.head = AttnHead{1, n_wide, n_narrow, 0};
+    if (tid == 0)
+        *ws.head = AttnHead{kPlanned, n_wide, n_narrow, R, (int32_t)a.n_tokens, a.n_heads, Hk, p.head_dim, p.n_seqs, p.table_width};
+}
+
+// A plan of this batch and pool is in the workspace: its lists, which say
+// where to read and write, are not looked at otherwise.
+__device__ __forceinline__ bool planned(const AttnArgs &a) {
+    const AttnHead h = *a.ws.head;
+    return h.magic == kPlanned && h.n_req == a.n_req && h.n_tokens == a.n_tokens && h.n_heads == a.n_heads &&
+           h.n_kv_heads * a.group == a.n_heads && h.head_dim == a.head_dim && h.n_seqs == a.n_seqs &&
+           h.table_width == a.table_width;
 }
 
 // ------------------------------------------------------------------ wide items
@@ -438,15 +445,15 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
         const int64_t from = (int64_t)page * a.page_stride + (int64_t)head * a.head_stride;
         const uint16_t *lk = lds + buf * kBuf + wave * kBlk * D, *lv = lk + 2 * kBuf;
 #pragma unroll
-        for (int i = 0; i < kPieces / 4; ++i) load_lds16_later(kp + from, k_at[i], lk + i * 512);
+        for (int i = 0; i < kPieces / 4; ++i) load_lds16(kp + from, k_at[i], lk + i * 512);
         if (t_first + kBlk <= end) {
 #pragma unroll
-            for (int i = 0; i < kPieces / 4; ++i) load_lds16_later(vp + from, v_at[i], lv + i * 512);
+            for (int i = 0; i < kPieces / 4; ++i) load_lds16(vp + from, v_at[i], lv + i * 512);
         } else {    // behind the end there may be anything, and zero times anything is to be zero
 #pragma unroll
             for (int i = 0; i < kPieces / 4; ++i) {
                 const char *v = reinterpret_cast<const char *>(vp + from) + v_at[i];
-                load_lds16_later(t_first + (i * 64 + lane) / kPieces < end ? v : reinterpret_cast<const char *>(zeros),
+                load_lds16(t_first + (i * 64 + lane) / kPieces < end ? v : reinterpret_cast<const char *>(zeros),
                                  lv + i * 512);
             }
         }
@@ -712,7 +719,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attn_items(AttnArgs a) {
     __shared__ __align__(1024) uint16_t lds[4 * kTileKv * D];
     __shared__ int lds_lim[4];
-    if (!a.ws.head->ok) return;
+    if (!planned(a)) return;
     const int n_wide = a.ws.head->n_wide, n_narrow = a.ws.head->n_narrow;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool wide_first = blockIdx.x < gridDim.x / 2;
@@ -735,9 +742,9 @@ __global__ __launch_bounds__(256, 2) void attn_items(AttnArgs a) {
 // A wave for kHeads heads of a query.  A lane weighs one part of one head, 64 /
 // kHeads parts at a time; the parts' values follow with 16 loads in flight.
 template <typename T, int D, int kHeads>
-__global__ __launch_bounds__(256) void attn_join(AttnArgs a, int32_t n_req) {
+__global__ __launch_bounds__(256) void attn_join(AttnArgs a) {
     constexpr int kParts = 64 / kHeads, kFly = 16 / kHeads, kPer = D / 64;
-    if (!a.ws.head->ok) return;
+    if (!planned(a)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per_query = (a.n_heads + kHeads - 1) / kHeads;
     const int64_t at = (int64_t)blockIdx.x * 4 + wave;
@@ -746,7 +753,7 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a, int32_t n_req) {
     if (t >= a.n_tokens) return;
     const int64_t q_row = a.ws.tok[t];
     const int j = a.ws.pos[t];
-    const AttnParts own = a.ws.parts[j], grp = a.ws.parts[n_req + j];
+    const AttnParts own = a.ws.parts[j], grp = a.ws.parts[a.n_req + j];
     if (own.chunks < 0) return;     // written already
     const int n = own.chunks + grp.chunks, heads = min(a.n_heads - h0, kHeads);
     auto row = [&](int c) -> int64_t {      // of head h0
@@ -815,13 +822,13 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a, int32_t n_req) {
 }
 
 template <typename T, int D>
-hipError_t launch(const AttnArgs &a, int32_t n_req, hipStream_t st) {
+hipError_t launch(const AttnArgs &a, hipStream_t st) {
     attn_items<T, D><<<512, 256, 0, st>>>(a);     // two workgroups to a CU
     // A wave to a row where that does no more than fill the chip; where there are many rows, mostly
     // of two parts, four rows to a wave have more loads in flight.
     const int64_t rows = a.n_tokens * a.n_heads, waves = a.n_tokens * ((a.n_heads + 3) / 4);
-    if (rows <= 16384) attn_join<T, D, 1><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a, n_req);
-    else attn_join<T, D, 4><<<(uint32_t)((waves + 3) / 4), 256, 0, st>>>(a, n_req);
+    if (rows <= 16384) attn_join<T, D, 1><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a);
+    else attn_join<T, D, 4><<<(uint32_t)((waves + 3) / 4), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -876,9 +883,9 @@ hipError_t launch_attn_plan(const AttnPlanArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-hipError_t launch_attn(const AttnArgs &a, int32_t n_req, int32_t head_dim, int32_t dtype, hipStream_t st) {
-    if (dtype == PC_BF16) return head_dim == 128 ? launch<Bf16, 128>(a, n_req, st) : launch<Bf16, 64>(a, n_req, st);
-    return head_dim == 128 ? launch<Fp16, 128>(a, n_req, st) : launch<Fp16, 64>(a, n_req, st);
+hipError_t launch_attn(const AttnArgs &a, int32_t dtype, hipStream_t st) {
+    if (dtype == PC_BF16) return a.head_dim == 128 ? launch<Bf16, 128>(a, st) : launch<Bf16, 64>(a, st);
+    return a.head_dim == 128 ? launch<Fp16, 128>(a, st) : launch<Fp16, 64>(a, st);
 }
 
 }  // namespace pcr

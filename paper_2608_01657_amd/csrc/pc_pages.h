@@ -66,9 +66,11 @@ struct AttnItem {
 struct AttnParts {
     int32_t base, chunks, n_tok, t0;
 };
+// What the plan was made for, and the sizes of its lists.
 struct AttnHead {
-    int32_t ok, n_wide, n_narrow, pad;
+    int32_t magic, n_wide, n_narrow, n_req, n_tokens, n_heads, n_kv_heads, head_dim, n_seqs, table_width;
 };
+constexpr int32_t kPlanned = 0x70634174;
 struct AttnWs {
     AttnHead *head;         // 256 bytes, with kZeroOffset bytes of zeros from there on
     int32_t *tok;           // [n_tokens] query row of the query at this place of the order
@@ -103,10 +105,11 @@ struct AttnArgs {
     int64_t page_stride, q_token, q_head, out_token, out_head;   // elements
     int32_t head_stride, token_stride;                           // of a page, elements
     int32_t table_width, n_pages, n_heads, group;                // group: query heads of a KV head
+    int32_t n_req, n_seqs, head_dim;
     float scale_log2;
     int64_t n_tokens;
     AttnWs ws;
 };
-hipError_t launch_attn(const AttnArgs &a, int32_t n_req, int32_t head_dim, int32_t dtype, hipStream_t st);
+hipError_t launch_attn(const AttnArgs &a, int32_t dtype, hipStream_t st);
 
 }  // namespace pcr

@@ -215,8 +215,11 @@ int32_t pc_attn(const pc_pages *pages, int32_t layer, const pc_rows *q, int32_t 
     a.n_heads = n_heads;
     a.group = n_heads / pages->n_kv_heads;
     a.scale_log2 = (float)(scale * 1.4426950408889634);
+    a.n_req = n_req;
+    a.n_seqs = pages->n_seqs;
+    a.head_dim = pages->head_dim;
     a.n_tokens = n_tokens;
-    return done(launch_attn(a, n_req, pages->head_dim, pages->dtype, static_cast<hipStream_t>(stream)), "pc_attn");
+    return done(launch_attn(a, pages->dtype, static_cast<hipStream_t>(stream)), "pc_attn");
 }
 
 }  // extern "C"

@@ -306,6 +306,64 @@ def test_bad_batches_set_the_status_and_write_nothing():
     b.near(batch.attend(1, b.q.to(DEV), lse=lse), lse, *b.exact())
 
 
+def test_without_a_plan_of_this_batch_nothing_is_written():
+    b = Batch(DECODE, 8, 2, 64, torch.bfloat16)
+    pool = b.upload()
+    R, T = len(b.rows), b.q.shape[0]
+    q, seq, q_off = b.q.to(DEV), b.seq.to(DEV), b.q_off.to(DEV)
+    batch = dv.PrefixBatch(pool, R, T, 8)
+    batch.workspace.fill_(1)
+    out = torch.full_like(q, 3.0)
+    batch.attend(1, q, out)                                  # no plan
+    assert (out == 3).all()
+    batch.plan(seq, q_off, *b.groups())
+    other = dv.PagePool(pool.k, pool.v, table=pool.table[:-1].contiguous(), length=pool.length[:-1].contiguous())
+    batch.pool = other
+    batch.attend(1, q, out)                                  # of a pool with fewer sequences
+    assert (out == 3).all()
+    batch.pool = pool
+    batch.n_heads = 4
+    wide = torch.full((T, 4, 64), 3.0, dtype=b.dtype, device=DEV)
+    batch.attend(1, q[:, :4], wide)                          # with fewer heads
+    assert (wide == 3).all()
+    batch.n_heads = 8
+    lse = torch.empty(q.shape[:2], device=DEV)
+    b.near(batch.attend(1, q, lse=lse), lse, *b.exact())
+
+
+def test_two_batches_of_a_pool_at_once():
+    """Batches with workspaces of their own, on two streams, and each again by itself."""
+    b = Batch(MANY, 16, 2, 128, torch.bfloat16)
+    pool = b.upload()
+    groups, q, seq, q_off = b.groups(), b.q.to(DEV), b.seq.to(DEV), b.q_off.to(DEV)
+    batches = [dv.PrefixBatch(pool, len(b.rows), q.shape[0], 16) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.empty_like(q) for _ in range(6)] for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(6):
+        for x in range(2):
+            batches[x].plan(seq, q_off, *(groups if x else ()), stream=streams[x])
+            batches[x].attend(1, q, outs[x][i], stream=streams[x])
+    torch.cuda.synchronize()
+    assert int(pool.status) == 0
+    o, z, tol, tol_z = b.exact()
+    for x in range(2):
+        assert all(torch.equal(outs[x][0], y) for y in outs[x])
+        lse = torch.empty(q.shape[:2], device=DEV)
+        again = batches[x].attend(1, q, lse=lse)
+        assert torch.equal(again, outs[x][0])
+        b.near(again, lse, o, z, tol, tol_z)
+
+
+def test_a_plan_for_thousands_of_requests():
+    """More requests than one pass of the planning workgroup; groups of two, many and one."""
+    rows = [((i // 2) if i < 1000 else 600 if i < 2400 else -1, 1 if i < 1000 else 2 if i < 2400 else 0, 1 + i % 3, 1)
+            for i in range(3000)]
+    b = Batch(rows, 2, 1, 64, torch.float16)
+    b.check()
+    b.check(grouped=False)
+
+
 def test_arguments_that_python_refuses():
     b = Batch(DECODE, 8, 2, 64, torch.bfloat16)
     pool = b.upload()
