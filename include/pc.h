@@ -275,7 +275,7 @@ int32_t pc_get_stats(const void *d_stats, int32_t n_inst, int32_t instance,
  * that change it must be ordered.
  *
  * Device-side status (d_status, one int32 in device memory that the caller
- * zeroes): a call that finds its lists or the pool's state out of range sets
+ * zeroes; pc_prefix_groups alone writes one of its own): a call that finds its lists or the pool's state out of range sets
  * it to PC_EINVAL, or PC_ENOPAGES, and does nothing else unless said
  * otherwise.  A call that finds it set does nothing, so that calls may be
  * queued one after another (or captured) and looked at once, at the end.
@@ -383,8 +383,10 @@ int32_t pc_pages_write(const pc_pages *pages, int32_t layer, const int32_t *d_se
  *   d_shared     [n_req] leading blocks with the same keys in all requests of
  *                group g; 0 for a group of one and behind the last group
  *   d_n_groups   [1]
- * n_req is at most PC_MAX_BATCH (else PC_EUNSUPPORTED).  d_status: PC_EINVAL
- * if the offsets fall, or leave [0, n_keys]. */
+ * n_req is at most PC_MAX_BATCH (else PC_EUNSUPPORTED), a request has 2^26
+ * blocks at most.  d_status, written by every call and not read: PC_OK, or
+ * PC_EINVAL where the offsets fall or leave [0, n_keys] (nothing else is written
+ * then). */
 int32_t pc_prefix_groups(const uint64_t *d_keys, int64_t n_keys, const int64_t *d_key_off, int32_t n_req,
                          int32_t min_blocks, int32_t *d_order, int32_t *d_group_off, int32_t *d_shared,
                          int32_t *d_n_groups, int32_t *d_status, void *stream);

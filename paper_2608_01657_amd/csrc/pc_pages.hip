@@ -224,6 +224,7 @@ struct FreeBits {
 // Scans a small pool by one workgroup; all its free pages.
 __device__ int scan_small(const pc_pages &p, FreeBits &f, int *lds) {
     const int lane = threadIdx.x & 63, words = (p.n_pages + 63) / 64;
+#pragma unroll 4
     for (int w = threadIdx.x >> 6; w < words; w += kThreads / 64) {
         const int page = w * 64 + lane;
         const uint64_t m = __ballot(page < p.n_pages && p.d_refs[page] == 0);
@@ -383,7 +384,8 @@ __global__ __launch_bounds__(kThreads) void extend_plan(pc_pages p, const int32_
     if (!kSmall) {
         if (threadIdx.x == 0) ws.head[0] = (int32_t)total;
     } else if (total) {
-        for (int page = threadIdx.x; page < p.n_pages; page += kThreads)
+        // the lowest ones: no further than the word with the last of them
+        for (int page = threadIdx.x; page < p.n_pages && free_bits.before[page >> 6] < total; page += kThreads)
             if (free_bits.is_free(page)) {
                 const int rank = free_bits.rank(page);
                 if (rank < total) {
@@ -590,7 +592,6 @@ __global__ __launch_bounds__(NT) void group_requests(const uint64_t *keys, int64
                                                      int32_t R, int32_t Rp, int32_t min_blocks, int32_t *order,
                                                      int32_t *group_off, int32_t *shared, int32_t *n_groups,
                                                      int32_t *status) {
-    if (*status != PC_OK) return;
     extern __shared__ __align__(16) uint64_t mark[];          // [Rp]
     int32_t *lead = reinterpret_cast<int32_t *>(mark + Rp);   // [Rp] then the sorted words
     int32_t *tab = lead + Rp;                                 // [2 Rp]
@@ -613,10 +614,8 @@ __global__ __launch_bounds__(NT) void group_requests(const uint64_t *keys, int64
         if (blocks[e] >= min_blocks) mark[i] = keys[a + min_blocks - 1];
     }
     __syncthreads();
-    if (any_bad) {
-        if (tid == 0) *status = PC_EINVAL;
-        return;
-    }
+    if (tid == 0) *status = any_bad ? PC_EINVAL : PC_OK;
+    if (any_bad) return;
     const uint32_t slots = 2 * Rp;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {

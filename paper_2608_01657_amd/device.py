@@ -405,7 +405,7 @@ def prefix_groups(keys, key_off, min_blocks: int = 1, stream=None) -> PrefixGrou
     R = key_off.numel() - 1
     _need(R >= 1, "key_off: n_req + 1 offsets")
     with _on(dev, stream):
-        g = PrefixGroups(*torch.zeros(3 * R + 3, dtype=torch.int32, device=dev).split((R, R + 1, R, 1, 1)))
+        g = PrefixGroups(*torch.empty(3 * R + 3, dtype=torch.int32, device=dev).split((R, R + 1, R, 1, 1)))
         pc_prefix_groups(keys, key_off, min_blocks, *g, stream)
     return g
 
