@@ -405,9 +405,10 @@ int32_t pc_prefix_groups(const uint64_t *d_keys, int64_t n_keys, const int64_t *
  *                 blocks have to hold the same tokens in all its requests: those
  *                 of the first one are read for all.  Shared blocks behind the
  *                 shortest request's last full one are taken as not shared.
- * A group's shared tokens are read once for the queries of all its requests,
- * each request's own tokens by itself, and long ranges in several parts; the
- * results are joined by their sums of exponentials.  Scores, sums and joined
+ * A group's shared tokens are read once for the queries of all its requests
+ * (where requests have many queries, or share little, also for each by itself,
+ * if that is sooner done), each request's own tokens by itself, and long ranges in
+ * several parts; the results are joined by their sums of exponentials.  Scores, sums and joined
  * values are in 32 bits; the weights are rounded to the pool's type before
  * the product with V.  Results do not depend on timing.
  * K of a token that a query does not see, and K and V behind the length, may

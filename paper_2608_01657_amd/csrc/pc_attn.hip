@@ -106,6 +106,14 @@ __device__ __forceinline__ int xcd_turns(int n) { return (n + 8 * kRun - 1) / (8
 
 constexpr int kPlanGroups = 16;
 
+// A group's shared tokens are read for all its members at once where the row
+// tiles that this saves, times the tokens, outweigh what the joint tiles cost:
+// partial results, written and joined.  Eight requests behind 4,096 shared
+// tokens, 8 of 32 heads' K and V, together / each by itself: 900 new tokens each
+// 462 / 409 us, 100: 70 / 69, 30: 35 / 39, 17: 23 / 26; decoding, 64 requests
+// behind 1,024 tokens 22 / 36, pairs behind 4,096 85 / 91, behind 1,024 38 / 37.
+constexpr int64_t kShareCost = 16 * kTileKv;
+
 // Sums of K words over the workgroup's threads: exclusive ones in v, those over
 // all in total.
 template <int NT, int K, typename N>
@@ -255,9 +263,12 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
         ws.pos[t] = j;
     }
     // the tokens that all members of a group share: by a thread for small groups, a wave for others
-    auto shared_tokens = [&](int g, int least) {
-        const int64_t tokens = least / kBlk * kBlk, blocks = share[g];
-        return blocks <= 0 ? 0 : (int)min(tokens, blocks * kBlk);
+    auto tiles_of = [&](int j) { return ((int64_t)(t0[j + 1] - t0[j]) * G + kWideRows - 1) / kWideRows; };
+    auto shared_tokens = [&](int g, int least, int64_t separate) {
+        const int64_t blocks = share[g], most = least / kBlk * kBlk;
+        const int64_t tokens = blocks <= 0 ? 0 : min(most, blocks * kBlk);
+        const int64_t joint = ((int64_t)(t0[goff[g + 1]] - t0[goff[g]]) * G + kWideRows - 1) / kWideRows;
+        return (separate - joint) * tokens > kShareCost * joint ? (int)tokens : 0;
     };
     for (int g = tid; g < n_groups; g += NT) {
         const int j0 = goff[g], j1 = goff[g + 1];
@@ -266,8 +277,12 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
             continue;
         }
         int least = 0x7fffffff;
-        for (int j = j0; j < j1; ++j) least = min(least, len[request(j)]);
-        const int tokens = j1 - j0 < 2 ? 0 : shared_tokens(g, least);
+        int64_t separate = 0;
+        for (int j = j0; j < j1; ++j) {
+            least = min(least, len[request(j)]);
+            separate += tiles_of(j);
+        }
+        const int tokens = j1 - j0 < 2 ? 0 : shared_tokens(g, least, separate);
         if (tokens)
             for (int j = j0; j < j1; ++j) place[j] = request(j) | g << 16;
         share[g] = tokens;
@@ -276,10 +291,17 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
     for (int i = wave; i < n_large; i += NT / 64) {
         const int g = large[i], j0 = goff[g], j1 = goff[g + 1];
         int least = 0x7fffffff;
-        for (int j = j0 + lane; j < j1; j += 64) least = min(least, len[request(j)]);
+        int64_t separate = 0;
+        for (int j = j0 + lane; j < j1; j += 64) {
+            least = min(least, len[request(j)]);
+            separate += tiles_of(j);
+        }
 #pragma unroll
-        for (int d = 32; d; d >>= 1) least = min(least, __shfl_xor(least, d));
-        const int tokens = shared_tokens(g, least);
+        for (int d = 32; d; d >>= 1) {
+            least = min(least, __shfl_xor(least, d));
+            separate += __shfl_xor(separate, d);
+        }
+        const int tokens = shared_tokens(g, least, separate);
         if (tokens)
             for (int j = j0 + lane; j < j1; j += 64) place[j] = request(j) | g << 16;
         if (lane == 0) share[g] = tokens;
@@ -730,7 +752,9 @@ __global__ __launch_bounds__(256, 2) void attn_items(AttnArgs a) {
                 if (which >= 0) wide_item<T, D>(a, a.ws.wide[which], lds, lds_lim);
             }
         } else {
-            for (int which = blockIdx.x + wave * gridDim.x; which < n_narrow; which += gridDim.x * 4)
+            // a wave an item, those of the workgroups that begin here first
+            const int half = gridDim.x / 2, first = wide_first ? 4 * half + (int)blockIdx.x : (int)blockIdx.x - half;
+            for (int which = first + wave * half; which < n_narrow; which += gridDim.x * 4)
                 narrow_item<T, D>(a, a.ws.narrow[which], lds + wave * kTileKv * D);
         }
         __syncthreads();

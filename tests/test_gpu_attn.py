@@ -175,6 +175,29 @@ def test_heads(rows, heads, kv_heads):
     Batch(rows, heads, kv_heads, 64, torch.float16, seed=heads, tokens_first=True).check()
 
 
+# groups that share enough for one pass over it: pairs, several, more rows than a tile, queries that
+# see only part of the shared tokens, one empty of own tokens
+SHARED = [(0, 70, 5, 1), (1, 90, 33, 1), (0, 70, 16, 1), (-1, 0, 70, 1), (1, 90, 1, 1), (2, 30, 40, 1), (2, 30, 1, 1),
+          (2, 30, 15, 3), (2, 30, 90, 2), (3, 65, 0, 9), (3, 65, 0, 1), (3, 65, 33, 33), (3, 65, 20, 60)]
+
+
+@pytest.mark.parametrize("heads,kv_heads", HEADS)
+@pytest.mark.parametrize("dtype,dim", [(torch.bfloat16, 128), (torch.float16, 64), (torch.bfloat16, 64)])
+def test_shared_prefixes(heads, kv_heads, dtype, dim):
+    b = Batch(SHARED, heads, kv_heads, dim, dtype, seed=heads, tokens_first=heads % 3 == 0)
+    b.check()
+    b.check(causal=False)
+    b.check(grouped=False)
+
+
+@pytest.mark.parametrize("members", [2, 3, 16, 17, 40])
+def test_group_sizes(members):
+    """Both ways that the plan goes through a group, tiles that are not full, the rule's both sides."""
+    for blocks in (1, 9, 64, 130):
+        rows = [(i % 2, blocks + i % 2, 1 + 5 * i % 37, 1 + (i == 3) * 4) for i in range(2 * members)] + [(-1, 0, 9, 1)]
+        Batch(rows, 8, 2, 64, torch.bfloat16, seed=members).check()
+
+
 @pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 257, 1023, 1025])
 def test_lengths(length):
     for new in {1, min(length, 2), min(length, 17), length}:
