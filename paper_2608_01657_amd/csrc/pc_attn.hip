@@ -95,6 +95,8 @@ __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)"
 // with an L2 of its own: runs of kRun neighbouring items (row tiles of the
 // same tokens) go to one XCD, and the runs round the XCDs, so that the long
 // items at the front of the list are spread over all.
+// (Whole eighths of the list to an XCD instead left half of the chip with the short items: prompts of
+// 900 tokens behind cached ones 274 us in place of 196.)
 constexpr int kRun = 8;
 __device__ __forceinline__ int xcd_item(int turn, int n) {
     const int k = turn >> 3, at = (k / kRun * 8 + (turn & 7)) * kRun + k % kRun;
@@ -178,8 +180,9 @@ __device__ __forceinline__ uint32_t divide(uint32_t x, uint32_t d) {
 // dependent reads away, and what comes after is kept in LDS, where each query
 // and each item finds its request or segment by a binary search.  Every
 // workgroup works all segments out by itself and writes its share of the
-// queries and items; the first one writes the rest.  (128 requests with 3,000
-// items: 20 us by one workgroup, most of it in writing items.)
+// queries and items; the first one writes the rest.  128 requests with 3,000
+// items took 20 us by one workgroup, most of it to write items; by 16 they take
+// 10.
 template <int NT>
 __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
     const pc_pages &p = a.p;
@@ -255,13 +258,6 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
     }
     if (tid == 0) t0[R] = before;
     __syncthreads();
-    // the queries in the order
-    for (int t = wg_tid; t < (int)a.n_tokens; t += wg_step) {
-        const int j = last_at(t0, R, t), i = t - t0[j], n = t0[j + 1] - t0[j], r = request(j);
-        ws.tok[t] = q_off[r] + i;
-        ws.lim[t] = a.causal ? len[r] - n + i + 1 : len[r];
-        ws.pos[t] = j;
-    }
     // the tokens that all members of a group share: by a thread for small groups, a wave for others
     auto tiles_of = [&](int j) { return ((int64_t)(t0[j + 1] - t0[j]) * G + kWideRows - 1) / kWideRows; };
     auto shared_tokens = [&](int g, int least, int64_t separate) {
@@ -359,9 +355,8 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
         x.part = direct ? -1 : rows_at + at[2];
         seg[tid] = x;
         first_item[tid] = at[0];
-        if (first && i < n_seg)     // own: at the request's place; groups': behind both lists, for now
-            ws.parts[i < n_groups ? 2 * R + i : i - n_groups] =
-                direct ? AttnParts{-1, -1, 0, 0} : AttnParts{x.part, chunks, x.n_tok, x.t0};
+        // by every workgroup, for itself
+        if (i < n_seg) ws.parts[i < n_groups ? R + i : i - n_groups] = AttnParts{x.part, direct ? -1 : chunks};
         __syncthreads();
         const int n_items = all[0], n_here = min(n_seg - i0, NT);
         for (int u = wg_tid; u < n_items; u += wg_step) {
@@ -379,9 +374,18 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
         rows_at += all[2];
         __syncthreads();
     }
+    // the queries in the order, and where their partial results are
+    for (int t = wg_tid; t < (int)a.n_tokens; t += wg_step) {
+        const int j = last_at(t0, R, t), r = request(j), g = group(j), n = t0[j + 1] - t0[j];
+        const AttnParts own = ws.parts[j], grp = g == kNoGroup ? AttnParts{0, 0} : ws.parts[R + g];
+        const int g0 = g == kNoGroup ? t : t0[goff[g]], gn = g == kNoGroup ? 0 : t0[goff[g + 1]] - g0;
+        const int q_row = q_off[r] + t - t0[j];
+        ws.tok[t] = q_row;
+        ws.lim[t] = a.causal ? len[r] - n + t - t0[j] + 1 : len[r];
+        ws.row[t] = AttnRow{q_row, own.chunks, own.base + (t - t0[j]) * a.n_heads, n * a.n_heads,
+                            grp.chunks, grp.base + (t - g0) * a.n_heads, gn * a.n_heads, 0};
+    }
     if (!first) return;
-    for (int j = tid; j < R; j += NT)
-        ws.parts[R + j] = group(j) == kNoGroup ? AttnParts{0, 0, 0, 0} : ws.parts[2 * R + group(j)];
     if (tid == 0)
         *ws.head = AttnHead{kPlanned, n_wide, n_narrow, R, (int32_t)a.n_tokens, a.n_heads, Hk, p.head_dim, p.n_seqs, p.table_width};
 }
@@ -412,7 +416,13 @@ __device__ __forceinline__ int swap_v_narrow(int t) { return D == 128 ? 2 * (t &
 // A workgroup of four waves takes 128 rows, a wave 32 of them (the columns of
 // 32 x 32 x 16 products), and 64 tokens of K and V at a time from LDS, where a
 // second pair of buffers fills meanwhile.  16-byte pieces of a token's row are
-// permuted in LDS (see swap_k and swap_v).
+// permuted in LDS (see swap_k and swap_v).  Prompts of 900 tokens behind 4,096
+// cached ones run at 790 TFLOP/s (a library's product of 8192^3: 1,206); the
+// matrix units are busy 37 % of the time, the vector units about as long (an
+// exponential takes the time of 512 products).  The two parts of a tile only
+// partly overlap between the two waves of a SIMD; eight waves in two teams that
+// barriers kept half a tile apart took 12 % longer, as the reads of LDS then
+// all fall into one half.
 template <typename T, int D>
 __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, uint16_t *lds, int *lds_lim) {
     constexpr int kPieces = D / 8, kSteps = D / 16, kDb = D / 32, kBuf = kTileKv * D;   // K, K, V, V
@@ -599,6 +609,8 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
 // (two pages) at a time, bound by memory.  K and V of the next tokens are
 // loaded to registers while the present ones are weighed and multiplied; V
 // goes on through a piece of LDS of the wave's own, for the transposing read.
+// Four decoding requests of 60,000 tokens: 4.7 TB/s with the join (a copy:
+// 5.2).  64 tokens at a time by loads straight to LDS: 3 % longer.
 template <typename T, int D>
 __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it, uint16_t *lv) {
     constexpr int kPieces = D / 8, kSteps = D / 32, kDb = D / 16, kStep = 32, kPages = kStep / kBlk;
@@ -768,22 +780,20 @@ __global__ __launch_bounds__(256, 2) void attn_items(AttnArgs a) {
 template <typename T, int D, int kHeads>
 __global__ __launch_bounds__(256) void attn_join(AttnArgs a) {
     constexpr int kParts = 64 / kHeads, kFly = 16 / kHeads, kPer = D / 64;
-    if (!planned(a)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per_query = (a.n_heads + kHeads - 1) / kHeads;
     const int64_t at = (int64_t)blockIdx.x * 4 + wave;
     const int64_t t = at / per_query;
     const int h0 = (int)(at - t * per_query) * kHeads;
     if (t >= a.n_tokens) return;
-    const int64_t q_row = a.ws.tok[t];
-    const int j = a.ws.pos[t];
-    const AttnParts own = a.ws.parts[j], grp = a.ws.parts[a.n_req + j];
-    if (own.chunks < 0) return;     // written already
-    const int n = own.chunks + grp.chunks, heads = min(a.n_heads - h0, kHeads);
+    const AttnRow x = a.ws.row[t];
+    if (!planned(a)) return;
+    if (x.own_chunks < 0) return;       // written already
+    const int64_t q_row = x.q_row;
+    const int n = x.own_chunks + x.grp_chunks, heads = min(a.n_heads - h0, kHeads);
     auto row = [&](int c) -> int64_t {      // of head h0
-        const AttnParts &x = c < grp.chunks ? grp : own;
-        const int k = c < grp.chunks ? c : c - grp.chunks;
-        return x.base + ((int64_t)k * x.n_tok + (t - x.t0)) * a.n_heads + h0;
+        return h0 + (c < x.grp_chunks ? x.grp_row + (int64_t)c * x.grp_step
+                                      : x.own_row + (int64_t)(c - x.grp_chunks) * x.own_step);
     };
     const int my_head = lane / kParts, my_part = lane % kParts;
     float top = kNegInf, sum = 0, o[kHeads][kPer];
@@ -848,8 +858,9 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a) {
 template <typename T, int D>
 hipError_t launch(const AttnArgs &a, hipStream_t st) {
     attn_items<T, D><<<512, 256, 0, st>>>(a);     // two workgroups to a CU
-    // A wave to a row where that does no more than fill the chip; where there are many rows, mostly
-    // of two parts, four rows to a wave have more loads in flight.
+    // A wave to a row where that does no more than fill the chip (2,700 rows of up to 36 parts: 10 us, by
+    // four rows to a wave 17 us); where there are many rows, mostly of two parts, four rows to a wave have
+    // more loads in flight (65,000 rows: 18 us, by one 38 us).
     const int64_t rows = a.n_tokens * a.n_heads, waves = a.n_tokens * ((a.n_heads + 3) / 4);
     if (rows <= 16384) attn_join<T, D, 1><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a);
     else attn_join<T, D, 4><<<(uint32_t)((waves + 3) / 4), 256, 0, st>>>(a);
@@ -872,15 +883,15 @@ int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_h
     if (rows > 0x7fffffff || wide > 0x7fffffff) return -1;
     int64_t o = 0;
     auto take = [&](int64_t bytes) { const int64_t at = o; o += up(bytes); return at; };
-    const int64_t head = take(256), tok = take(4 * n_tokens), lim = take(4 * n_tokens), pos = take(4 * n_tokens),
-                  parts = take(3LL * n_req * (int64_t)sizeof(AttnParts)),
+    const int64_t head = take(256), tok = take(4 * n_tokens), lim = take(4 * n_tokens), row = take(n_tokens * (int64_t)sizeof(AttnRow)),
+                  parts = take(2LL * n_req * (int64_t)sizeof(AttnParts)),
                   w = take(wide * (int64_t)sizeof(AttnItem)), nr = take(narrow * (int64_t)sizeof(AttnItem)),
                   po = take(rows * head_dim * 4), pl = take(rows * 4);
     if (ws) {
         ws->head = reinterpret_cast<AttnHead *>(base + head);
         ws->tok = reinterpret_cast<int32_t *>(base + tok);
         ws->lim = reinterpret_cast<int32_t *>(base + lim);
-        ws->pos = reinterpret_cast<int32_t *>(base + pos);
+        ws->row = reinterpret_cast<AttnRow *>(base + row);
         ws->parts = reinterpret_cast<AttnParts *>(base + parts);
         ws->wide = reinterpret_cast<AttnItem *>(base + w);
         ws->narrow = reinterpret_cast<AttnItem *>(base + nr);
@@ -893,7 +904,8 @@ int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_h
 
 hipError_t launch_attn_plan(const AttnPlanArgs &a, hipStream_t st) {
     const size_t bytes = 4 * (7 * (size_t)a.n_req + 3);
-    // a barrier and a sum over 16 wavefronts cost more than what few requests have to do
+    // A barrier and a sum over 16 wavefronts cost more than what few requests have to do: with 256 / 1,024
+    // threads, one request 6.7 / 9.1 us, 64 8.7 / 11.2 us, 256 11.4 / 12.0 us, 512 15.4 / 13.1 us.
     if (a.n_req <= 256) {
         attn_plan<256><<<kPlanGroups, 256, bytes, st>>>(a);
         return hipGetLastError();

@@ -48,7 +48,10 @@ constexpr int kTileKv = 64;          // tokens of K and V that a wide tile takes
 constexpr int kWideRows = 128;       // query rows of a wide tile
 constexpr int kNarrowRows = 16;      // query rows of a narrow tile
 // Items that the plan aims at where it splits a long axis, and the fewest
-// 64-token blocks of an item that it splits down to.
+// 64-token blocks of an item that it splits down to.  More items fill the chip
+// more evenly, fewer have less to write and to join: 128 requests behind 8,192
+// shared tokens take 84 us with 512 and 2,048 (a workgroup and a wave for every
+// place on the chip), 75 us with these; four of 60,000 tokens 112 and 104 us.
 constexpr int kWideItems = 256, kNarrowItems = 1024;
 constexpr int kWideMinBlocks = 4, kNarrowMinBlocks = 2;
 
@@ -62,9 +65,15 @@ struct AttnItem {
     int32_t part;           // partial row of (first query, head 0); -1: straight to the output
     int32_t pad;
 };
-// Where a request's partial results are: its own tokens' and its group's.
+// Where a segment's partial results are: their first row, and how many parts
+// each query has (-1: they go straight to the output).
 struct AttnParts {
-    int32_t base, chunks, n_tok, t0;
+    int32_t base, chunks;
+};
+// The same for a query: its own tokens' parts and its group's, of head 0, and
+// the rows from a part to the next.
+struct AttnRow {
+    int32_t q_row, own_chunks, own_row, own_step, grp_chunks, grp_row, grp_step, pad;
 };
 // What the plan was made for, and the sizes of its lists.
 struct AttnHead {
@@ -75,8 +84,8 @@ struct AttnWs {
     AttnHead *head;         // 256 bytes, with kZeroOffset bytes of zeros from there on
     int32_t *tok;           // [n_tokens] query row of the query at this place of the order
     int32_t *lim;           // [n_tokens] it sees the tokens before this one
-    int32_t *pos;           // [n_tokens] its request's place in the order
-    AttnParts *parts;       // [3][n_req]: own, group, and groups by number
+    AttnRow *row;           // [n_tokens]
+    AttnParts *parts;       // [2][n_req]: of the requests at their places, of groups
     AttnItem *wide, *narrow;
     float *o;               // [rows][head_dim] partial results, normalised
     float *lse;             // [rows] log2 of their sums of exponentials

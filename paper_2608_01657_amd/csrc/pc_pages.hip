@@ -75,7 +75,8 @@ __device__ bool bad_list(const pc_pages &p, const int32_t *seq, int32_t n, uint3
 
 // ------------------------------------------------------------------ copies
 
-// 16 bytes a thread; page_elems is a multiple of 8.
+// 16 bytes a thread at a time.  Bound by memory: pages of 12 layers are copied at 5.5 TB/s (512 branches
+// of 64 sequences), moved at 5.0 TB/s (2,000 pages of 786 KB), read and write together.
 __device__ __forceinline__ void copy_page(const pc_pages &p, int which, int src, int dst) {
     const int64_t layer = (int64_t)(which >> 1) * p.layer_stride;
     uint16_t *base = static_cast<uint16_t *>((which & 1) ? p.d_v : p.d_k) + layer;
@@ -156,8 +157,7 @@ __global__ __launch_bounds__(256) void free_pages(pc_pages p, const int32_t *seq
     if (threadIdx.x == 0) p.d_len[s] = 0;
 }
 
-// Both steps by one workgroup, a wave to a sequence: fewer launches, where
-// there are few table entries to look at.
+// Both steps by one workgroup, a wave to a sequence (see kFewEntries).
 __global__ __launch_bounds__(kThreads) void fork_or_free_few(pc_pages p, const int32_t *seq, const int32_t *child,
                                                              int32_t n, int32_t *status) {
     extern __shared__ uint32_t seen[];
@@ -205,10 +205,13 @@ __global__ __launch_bounds__(256) void scan_refs(pc_pages p, PagesWs ws, const i
     if (threadIdx.x == 0) ws.chunk_free[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
 }
 
-// A pool of so many pages or fewer is scanned by the one workgroup that plans,
-// in place of two kernels of their own: 2 us less than their launches take at
-// 512 pages, even at 16,384.
+// A pool of so many pages or fewer is scanned by the one workgroup that plans;
+// larger ones by kernels of their own before and after it.  A call that finds
+// nothing to copy, one way / the other: 512 pages 7.3 / 11.4 us (extend) and 5.6 /
+// 11.2 us (compact), 16,384 pages 10.2 / 12.6 and 12.5 / 17.0, 65,536 pages 19.4 /
+// 12.5 and 35.8 / 17.2.
 constexpr int kSmallPool = 16384;
+static_assert(kSmallPool / 64 <= kThreads, "a thread for each word");
 
 // Free pages as bits, with those before each word.
 struct FreeBits {
@@ -759,9 +762,10 @@ int64_t pages_ws(const pc_pages &p, int64_t n, char *base, PagesWs *ws) {
 
 static size_t seen_bytes(const pc_pages &p) { return (size_t)((p.n_seqs + 31) / 32) * 4; }
 
-// Table entries up to which one workgroup forks or frees by itself: 2 us less
-// than two launches for a few sequences, as long at 8,192 entries.
-constexpr int64_t kFewEntries = 8192;
+// Table entries up to which one workgroup forks or frees by itself.  A fork and
+// a free of n sequences by it / by two kernels each: 4 of 16 blocks 5.5 / 7.9 us,
+// 16 of 64 6.5 / 8.0 us, 64 of 64 15.0 / 8.3 us.
+constexpr int64_t kFewEntries = 1024;
 
 hipError_t launch_fork(const pc_pages &p, const int32_t *parent, const int32_t *child, int32_t n, int32_t *status,
                        hipStream_t st) {
@@ -813,7 +817,8 @@ hipError_t launch_compact(const pc_pages &p, int32_t *refs_to, int32_t *table_to
 hipError_t launch_write(const pc_pages &p, int32_t layer, const int32_t *seq, const int32_t *new_off, int32_t n,
                         int64_t n_tokens, const pc_rows &k_new, const pc_rows &v_new, int32_t *status, hipStream_t st) {
     // workgroups enough for the case that one sequence has all the tokens, but not many more than the chip
-    // holds at a time
+    // holds at a time (22,000 tokens of 12 sequences: 2,048 41.3 us, 8,192 39.6 us, 32,768 50.2 us; bound by
+    // memory, 4.4 TB/s)
     int64_t y = (n_tokens * p.n_kv_heads * (p.head_dim / 8) + 255) / 256;
     const int64_t most = 8192 / n > 1 ? 8192 / n : 1;
     y = y < 1 ? 1 : y > most ? most : y;
@@ -837,7 +842,9 @@ hipError_t launch_groups(const uint64_t *keys, int64_t n_keys, const int64_t *ke
                                           n_groups, status);
         return hipGetLastError();
     };
-    // no more registers to sort than requests need (four a thread for 1,024 of them: 22 us)
+    // No more registers to sort than requests need: with four a thread, 1,024 of them took 22 us in place
+    // of 13.  256 threads for few, whose barriers and sums cost less: 8 requests 6.4 us in place of 7.0, 256
+    // 11.2 in place of 12.2 (both kernels).
     const hipError_t e = rp <= 256    ? launch(&group_requests<256, 1>, 256)
                          : rp <= 1024 ? launch(&group_requests<1024, 1>, 1024)
                          : rp <= 2048 ? launch(&group_requests<1024, 2>, 1024)
