@@ -417,12 +417,15 @@ __device__ __forceinline__ int swap_v_narrow(int t) { return D == 128 ? 2 * (t &
 // 32 x 32 x 16 products), and 64 tokens of K and V at a time from LDS, where a
 // second pair of buffers fills meanwhile.  16-byte pieces of a token's row are
 // permuted in LDS (see swap_k and swap_v).  Prompts of 900 tokens behind 4,096
-// cached ones run at 790 TFLOP/s (a library's product of 8192^3: 1,206); the
-// matrix units are busy 37 % of the time, the vector units about as long (an
-// exponential takes the time of 512 products).  The two parts of a tile only
-// partly overlap between the two waves of a SIMD; eight waves in two teams that
-// barriers kept half a tile apart took 12 % longer, as the reads of LDS then
-// all fall into one half.
+// cached ones run at 790 TFLOP/s (a library's product of 8192^3, which the
+// chip's power bounds too: 1,206 to 1,380).  The matrix units are busy 38 % of the time and the
+// vector units about as long; the products left out, the same prompts take 87
+// us in place of 140, and no single part of the weights' work more than 12 us
+// (the exponentials).  What did not help: eight waves in two teams that barriers
+// kept half a tile apart (12 % longer), a wave that weighed one half of a tile
+// between the products of the others (1 % longer), tiles of 32 tokens (6 %),
+// wave priorities (the same).  Products of four independent sums in turn, their
+// reads issued four products ahead, save 2 %.
 template <typename T, int D>
 __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, uint16_t *lds, int *lds_lim) {
     constexpr int kPieces = D / 8, kSteps = D / 16, kDb = D / 32, kBuf = kTileKv * D;   // K, K, V, V
@@ -510,20 +513,17 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
         }
         const uint16_t *lk = lds + (n & 1) * kBuf, *lv = lk + 2 * kBuf;
         f32x16 s[2];
-        // the wave that multiplies goes before the one that weighs (3.5 % less time on long prompts;
-        // the same around the second product costs 3 %)
-        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[h][r] = 0;
 #pragma unroll
-            for (int st = 0; st < kSteps; ++st) {
+        for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
                 const int at = (h * 32 + col) * D + (((2 * st + half) ^ swap_k<D>(col)) * 8);
                 s[h] = T::mma32(*reinterpret_cast<const s16x8 *>(lk + at), qf[st], s[h]);
             }
-        }
-        __builtin_amdgcn_s_setprio(0);
         const int base = it.kv0 + n * kTileKv;
         if (base + kTileKv > least) {
 #pragma unroll
@@ -567,13 +567,21 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
         const int quad = (lane >> 2) & 3, g16 = (lane >> 4) & 1;
         const int vt = 4 * half + quad;     // token of this lane's address, within eight
 #pragma unroll
-        for (int i = 0; i < kDb; ++i) {
-            const int piece = (4 * i + 2 * g16 + ((lane & 3) >> 1)) ^ swap_v<D>(vt);
-            const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
+        for (int st = 0; st < 4; ++st)
 #pragma unroll
-            for (int st = 0; st < 4; ++st)
+            for (int i = 0; i < kDb; ++i) {
+                const int piece = (4 * i + 2 * g16 + ((lane & 3) >> 1)) ^ swap_v<D>(vt);
+                const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
                 o[i] = T::mma32(join(read_tr(v + st * 16 * D), read_tr(v + (st * 16 + 8) * D)), pf[st], o[i]);
+            }
+        // four products' reads ahead of the first one
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
+#pragma unroll
+        for (int i = 0; i < 4 * kDb - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
     }
     l += __shfl_xor(l, 32);
     if (active) {

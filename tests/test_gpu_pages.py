@@ -147,6 +147,37 @@ def test_random_traffic(seed):
         t.check()
 
 
+@pytest.mark.parametrize("n_pages", [63, 64, 65, 4095, 4096, 4097, 16383, 16384, 16385, 20481])
+def test_pool_sizes(n_pages):
+    """Both ways of scanning a pool, at the edges of its words, chunks and of the small pool; full and empty pools."""
+    width = n_pages // 6 + 1
+    t = Pair(n_pages, 9, width, layers=1, heads=1)
+    sizes = [n_pages // 6, n_pages // 3 % width, 5, n_pages // 7]
+    t.extend([3, 1, 0, 2], [16 * n for n in sizes])
+    t.extend([4], [1])
+    t.free([3, 0])
+    t.compact()
+    t.check()
+    t.fork([1, 2, 4], [5, 6, 7])
+    t.extend([5, 7, 8], [0, 3, 16 * (n_pages // 6)])
+    t.free([1, 2])
+    t.check()
+    t.compact()
+    t.check()
+    left = sum(r == 0 for r in t.model.refs)
+    while left:             # the last pages of the pool
+        n = min(left, width)
+        seq = next(s for s in range(9) if not t.model.len[s])
+        t.extend([seq], [16 * n - 7])
+        left -= n
+    t.check()
+    t.compact()             # nothing to move
+    t.extend([4], [16])     # and none left
+    t.free(list(range(9)))
+    t.compact()
+    t.check()
+
+
 def test_who_copies_a_shared_page():
     """All holders grow: the first in the list keeps the page.  Some do not: every one that grows copies."""
     t = Pair(64, 8, 4)
