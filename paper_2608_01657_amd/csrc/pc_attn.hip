@@ -42,6 +42,10 @@ struct Bf16 {
     static __device__ uint32_t pack(float a, float b) {
         return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
     }
+    // what pack() left of the two
+    static __device__ uint32_t pack_rest(float a, float b, uint32_t packed) {
+        return pack(a - __builtin_bit_cast(float, packed << 16), b - __builtin_bit_cast(float, packed & 0xffff0000u));
+    }
 };
 struct Fp16 {
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
@@ -53,6 +57,10 @@ struct Fp16 {
     }
     static __device__ uint32_t pack(float a, float b) {
         return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
+    }
+    static __device__ uint32_t pack_rest(float a, float b, uint32_t packed) {
+        const f16x2 p = __builtin_bit_cast(f16x2, packed);
+        return pack(a - (float)p[0], b - (float)p[1]);
     }
 };
 
@@ -707,7 +715,7 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
             m = now;
         }
         const float use = m == kNegInf ? 0.f : m;
-        union { uint32_t u[2 * kPages]; s16x8 v[kPages / 2]; } w;
+        union { uint32_t u[2 * kPages]; s16x8 v[kPages / 2]; } w, rest;
 #pragma unroll
         for (int h = 0; h < kPages; ++h) {
 #pragma unroll
@@ -717,6 +725,10 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
             }
             w.u[2 * h] = T::pack(s[h][0], s[h][1]);
             w.u[2 * h + 1] = T::pack(s[h][2], s[h][3]);
+            // here the matrix units wait for memory: the weights go in two pieces, so that they are exact to
+            // twice the type's bits
+            rest.u[2 * h] = T::pack_rest(s[h][0], s[h][1], w.u[2 * h]);
+            rest.u[2 * h + 1] = T::pack_rest(s[h][2], s[h][3], w.u[2 * h + 1]);
         }
         const int vt = 4 * quarter + ((lane >> 2) & 3);     // token of this lane's address, within a page
 #pragma unroll
@@ -724,8 +736,11 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
             const int piece = (2 * i + ((lane & 3) >> 1)) ^ swap_v_narrow<D>(vt);
             const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
 #pragma unroll
-            for (int h = 0; h < kPages; h += 2)
-                o[i] = T::mma16(join(read_tr(v + h * kBlk * D), read_tr(v + (h + 1) * kBlk * D)), w.v[h / 2], o[i]);
+            for (int h = 0; h < kPages; h += 2) {
+                const s16x8 vt8 = join(read_tr(v + h * kBlk * D), read_tr(v + (h + 1) * kBlk * D));
+                o[i] = T::mma16(vt8, w.v[h / 2], o[i]);
+                o[i] = T::mma16(vt8, rest.v[h / 2], o[i]);
+            }
         }
     }
     l += __shfl_xor(l, 16);
