@@ -17,6 +17,7 @@
 // matrix instruction's k is taken to be the order in which the first product
 // leaves them.  V^T comes from row-major V by the transposing LDS read.
 #include "pc_pages.h"
+#include "pc_wave.h"
 
 namespace pcr {
 
@@ -124,43 +125,6 @@ constexpr int kPlanGroups = 16;
 // behind 1,024 tokens 22 / 36, pairs behind 4,096 85 / 91, behind 1,024 38 / 37.
 constexpr int64_t kShareCost = 16 * kTileKv;
 
-// Sums of K words over the workgroup's threads: exclusive ones in v, those over
-// all in total.
-template <int NT, int K, typename N>
-__device__ __forceinline__ void plan_sum(N (&v)[K], N (&total)[K], N *lds) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    N x[K];
-#pragma unroll
-    for (int i = 0; i < K; ++i) x[i] = v[i];
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-        for (int i = 0; i < K; ++i) {
-            const N y = __shfl_up(x[i], d);
-            x[i] += lane >= d ? y : 0;
-        }
-    __syncthreads();
-    if (lane == 63)
-#pragma unroll
-        for (int i = 0; i < K; ++i) lds[w * K + i] = x[i];
-    __syncthreads();
-    N t[NT / 64][K];
-#pragma unroll
-    for (int k = 0; k < NT / 64; ++k)
-#pragma unroll
-        for (int i = 0; i < K; ++i) t[k][i] = lds[k * K + i];
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-        v[i] = x[i] - v[i];
-        total[i] = 0;
-#pragma unroll
-        for (int k = 0; k < NT / 64; ++k) {
-            v[i] += k < w ? t[k][i] : 0;
-            total[i] += t[k][i];
-        }
-    }
-}
-
 // A segment as the plan holds it: segment i < n_req is the own tokens of the
 // request at place i of the order, segment n_req + g group g's shared tokens.
 struct Segment {
@@ -260,7 +224,7 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
         const int j = j0 + tid;
         int n[1] = {0}, all[1];
         if (j < R) n[0] = q_off[request(j) + 1] - q_off[request(j)];
-        plan_sum<NT>(n, all, lds);
+        block_scan<NT>(n, all, lds);
         if (j < R) t0[j] = before + n[0];
         before += all[0];
     }
@@ -300,11 +264,9 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
             least = min(least, len[request(j)]);
             separate += tiles_of(j);
         }
+        separate = wave_last(wave_scan(separate));
 #pragma unroll
-        for (int d = 32; d; d >>= 1) {
-            least = min(least, __shfl_xor(least, d));
-            separate += __shfl_xor(separate, d);
-        }
+        for (int d = 32; d; d >>= 1) least = min(least, __shfl_xor(least, d));
         const int tokens = shared_tokens(g, least, separate);
         if (tokens)
             for (int j = j0 + lane; j < j1; j += 64) place[j] = request(j) | g << 16;
@@ -332,7 +294,7 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
         if (rows > kNarrowRows) work[0] += (rows + kWideRows - 1) / kWideRows * blocks;
         else if (rows) work[1] += blocks;
     }
-    plan_sum<NT>(work, all_work, lds64);
+    block_scan<NT>(work, all_work, lds64);
     const int64_t by_wide = (all_work[0] * Hk + kWideItems - 1) / kWideItems,
                   by_narrow = (all_work[1] * Hk + kNarrowItems - 1) / kNarrowItems;
     const int len_wide = (int)(by_wide < kWideMinBlocks ? kWideMinBlocks : by_wide);
@@ -358,7 +320,7 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
         const int items = chunks * x.tiles * Hk;
         // items of this pass, the wide ones among them, partial rows
         int at[3] = {items, is_wide ? items : 0, direct ? 0 : chunks * x.n_tok * a.n_heads}, all[3];
-        plan_sum<NT>(at, all, lds);
+        block_scan<NT>(at, all, lds);
         x.first = is_wide ? n_wide + at[1] : -1 - (n_narrow + at[0] - at[1]);
         x.part = direct ? -1 : rows_at + at[2];
         seg[tid] = x;

@@ -8,6 +8,7 @@
 // does not matter; new pages go by rank among the free ones, so results do not
 // depend on timing.
 #include "pc_pages.h"
+#include "pc_wave.h"
 
 namespace pcr {
 
@@ -21,31 +22,6 @@ __device__ __forceinline__ bool page_ok(const pc_pages &p, int page) { return (u
 
 __device__ __forceinline__ bool len_ok(const pc_pages &p, int len) {
     return len >= 0 && (int64_t)len <= (int64_t)p.table_width * kBlk;
-}
-
-// Exclusive sum over the workgroup's NT threads; *total: over all of them.
-template <int NT, typename N>
-__device__ N block_sum(N v, N *total, N *lds) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    N x = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const N y = __shfl_up(x, d);
-        x += lane >= d ? y : 0;
-    }
-    __syncthreads();
-    if (lane == 63) lds[w] = x;
-    __syncthreads();
-    N t[NT / 64], before = 0, all = 0;
-#pragma unroll
-    for (int i = 0; i < NT / 64; ++i) t[i] = lds[i];
-#pragma unroll
-    for (int i = 0; i < NT / 64; ++i) {
-        before += i < w ? t[i] : 0;
-        all += t[i];
-    }
-    *total = all;
-    return before + x - v;
 }
 
 // Whether the status was set when the workgroup began: one read for all its
