@@ -279,8 +279,9 @@ int32_t pc_get_stats(const void *d_stats, int32_t n_inst, int32_t instance,
  * it to PC_EINVAL, or PC_ENOPAGES, and does nothing else unless said
  * otherwise.  A call that finds it set does nothing, so that calls may be
  * queued one after another (or captured) and looked at once, at the end.
- * No call reads or writes outside the buffers described here, whatever the
- * lists and tables hold.
+ * Calls that may overlap (on other streams) have a status of their own each, or
+ * may be stopped by each other's errors.  No call reads or writes outside the
+ * buffers described here, whatever the lists and tables hold.
  *
  * Every call can be captured into a HIP graph.  A workspace holds nothing
  * between calls (but for pc_attn, see there): calls that do not overlap may

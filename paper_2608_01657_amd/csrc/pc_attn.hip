@@ -78,6 +78,11 @@ __device__ __forceinline__ void load_lds16(const void *g, const void *l) {
     const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const as3 *)l);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(g) : "memory", "m0");
 }
+__device__ __forceinline__ void load_lds16(const void *base, uint32_t offset, const void *l) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const as3 *)l);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base)
+                 : "memory", "m0");
+}
 __device__ __forceinline__ s16x4 read_tr(const uint16_t *l) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)l);
 }
@@ -86,11 +91,6 @@ __device__ __forceinline__ s16x8 join(s16x4 a, s16x4 b) {
 }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
-__device__ __forceinline__ void load_lds16(const void *base, uint32_t offset, const void *l) {
-    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const as3 *)l);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base)
-                 : "memory", "m0");
-}
 
 // The running maximum follows the scores only where they pass it by this much
 // (in powers of two): weights up to 2^8 lose nothing in any of the types, and
@@ -202,9 +202,11 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
         bad |= r >= (uint32_t)R || (atomicOr(&seen[r >> 5], 1u << (r & 31)) >> (r & 31) & 1);
         place[i] = (r < (uint32_t)R ? r : 0) | kNoGroup << 16;
     }
-    if (tid == 0) stop = status;        // another workgroup may set it meanwhile
+    // Only the first workgroup, which says in the end that there is a plan, goes by the status: another call may set
+    // it meanwhile, and either all of the plan is there or nobody follows it.
+    if (tid == 0) stop = first && status != PC_OK;
     __syncthreads();
-    if (stop != PC_OK) return;
+    if (stop) return;
     // every request once, and their queries one behind the other: every query in one of them
     for (int i = tid; i < R; i += NT) bad |= q_off[i + 1] < q_off[i];
     bad |= q_off[0] != 0 || q_off[R] != a.n_tokens;

@@ -24,7 +24,7 @@ struct PagesWs {
     int32_t *moved;         // [n_pages] compact: the page that moves to it
     int32_t *rank;          // [n_pages] compact: rank of a page that moves
     int32_t *entry;         // [4][n] extend: first new rank, pages held before, new pages, copied page or -1
-    int32_t *head;          // [4] extend: new pages; compact: pages in use, pages that move, -, whether to act
+    int32_t *head;          // [4] extend: new pages; compact: pages in use, pages that move; [3]: whether to act
     int32_t n_chunks;
 };
 int64_t pages_ws(const pc_pages &p, int64_t n_list, char *base, PagesWs *ws);

@@ -6,7 +6,9 @@
 // acts, and the second does nothing where the first set the status: a call
 // happens whole or not at all.  Counts change by integer atomics, whose order
 // does not matter; new pages go by rank among the free ones, so results do not
-// depend on timing.
+// depend on timing.  Where there is a workspace, the kernels behind the check go
+// by a word in it, written by one workgroup, and not by the status, which
+// another call may set meanwhile.
 #include "pc_pages.h"
 #include "pc_wave.h"
 
@@ -163,8 +165,7 @@ __global__ __launch_bounds__(kThreads) void fork_or_free_few(pc_pages p, const i
 // ------------------------------------------------------------------ free pages
 
 // Bitmap and count of a chunk's free pages.
-__global__ __launch_bounds__(256) void scan_refs(pc_pages p, PagesWs ws, const int32_t *status) {
-    if (*status != PC_OK) return;
+__global__ __launch_bounds__(256) void scan_refs(pc_pages p, PagesWs ws) {
     __shared__ int32_t sums[4];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int base = blockIdx.x * kChunkPages + w * (kChunkPages / 4);
@@ -257,7 +258,8 @@ __device__ int sum_chunks(const PagesWs &ws, int *lds) {
 template <bool kSmall>
 __global__ __launch_bounds__(kThreads) void extend_plan(pc_pages p, const int32_t *seq, const int32_t *add, int32_t n,
                                                         PagesWs ws, int32_t *status) {
-    if (*status != PC_OK) return;
+    if (threadIdx.x == 0) ws.head[3] = 0;
+    if (stopped(status)) return;
     constexpr int kPer = PC_MAX_BATCH / kThreads;
     extern __shared__ uint32_t seen[];
     __shared__ FreeBits free_bits;
@@ -360,9 +362,11 @@ __global__ __launch_bounds__(kThreads) void extend_plan(pc_pages p, const int32_
         if (threadIdx.x == 0) *status = PC_ENOPAGES;
         return;
     }
-    if (!kSmall) {
-        if (threadIdx.x == 0) ws.head[0] = (int32_t)total;
-    } else if (total) {
+    if (threadIdx.x == 0) {
+        ws.head[0] = (int32_t)total;
+        ws.head[3] = 1;
+    }
+    if (kSmall && total) {
         // the lowest ones: no further than the word with the last of them
         for (int page = threadIdx.x; page < p.n_pages && free_bits.before[page >> 6] < total; page += kThreads)
             if (free_bits.is_free(page)) {
@@ -376,8 +380,8 @@ __global__ __launch_bounds__(kThreads) void extend_plan(pc_pages p, const int32_
 }
 
 // The free pages of rank < head[0], listed by rank; they have a holder now.
-__global__ __launch_bounds__(256) void list_free(pc_pages p, PagesWs ws, const int32_t *status) {
-    if (*status != PC_OK) return;
+__global__ __launch_bounds__(256) void list_free(pc_pages p, PagesWs ws) {
+    if (ws.head[3] == 0) return;
     __shared__ FreeBits f;
     __shared__ int lds[4];
     const int total = ws.head[0], base = blockIdx.x * kChunkPages;
@@ -394,8 +398,8 @@ __global__ __launch_bounds__(256) void list_free(pc_pages p, PagesWs ws, const i
 }
 
 __global__ __launch_bounds__(256) void extend_pages(pc_pages p, const int32_t *seq, const int32_t *add, int32_t n,
-                                                    PagesWs ws, const int32_t *status) {
-    if (*status != PC_OK) return;
+                                                    PagesWs ws) {
+    if (ws.head[3] == 0) return;
     const int i = blockIdx.x;
     const int first = ws.entry[i], have = ws.entry[n + i], fresh = ws.entry[2 * n + i], src = ws.entry[3 * n + i];
     if (blockIdx.y == 0) {
@@ -424,10 +428,8 @@ __device__ __forceinline__ void list_move(const PagesWs &ws, int page, bool is_f
 // One workgroup: pages in use, and how many of them lie behind that number.
 template <bool kSmall>
 __global__ __launch_bounds__(kThreads) void compact_plan(pc_pages p, PagesWs ws, int32_t *n_live, const int32_t *status) {
-    if (*status != PC_OK) {
-        if (threadIdx.x == 0) ws.head[3] = 0;
-        return;
-    }
+    if (threadIdx.x == 0) ws.head[3] = 0;
+    if (stopped(status)) return;
     __shared__ FreeBits free_bits;
     __shared__ int lds[16];
     const int live = p.n_pages - (kSmall ? scan_small(p, free_bits, lds) : sum_chunks(ws, lds));
@@ -461,8 +463,8 @@ __global__ __launch_bounds__(kThreads) void compact_plan(pc_pages p, PagesWs ws,
     }
 }
 
-__global__ __launch_bounds__(256) void list_moves(pc_pages p, PagesWs ws, const int32_t *status) {
-    if (*status != PC_OK) return;
+__global__ __launch_bounds__(256) void list_moves(pc_pages p, PagesWs ws) {
+    if (ws.head[3] == 0) return;
     __shared__ FreeBits f;
     __shared__ int lds[4];
     const int live = ws.head[0], holes = ws.head[1], base = blockIdx.x * kChunkPages;
@@ -473,7 +475,7 @@ __global__ __launch_bounds__(256) void list_moves(pc_pages p, PagesWs ws, const 
 
 __global__ __launch_bounds__(256) void compact_pages(pc_pages p, int32_t *refs_to, int32_t *table_to, PagesWs ws,
                                                      int32_t *status) {
-    if (ws.head[3] == 0) return;    // the status that compact_plan saw; this kernel sets it itself
+    if (ws.head[3] == 0) return;
     const int live = ws.head[0], moves = ws.head[1];
     const int64_t copies = (int64_t)moves * 2 * p.n_layers;
     for (int64_t u = blockIdx.x; u < copies; u += gridDim.x) {
@@ -769,11 +771,11 @@ hipError_t launch_extend(const pc_pages &p, const int32_t *seq, const int32_t *a
     if (p.n_pages <= kSmallPool) {
         extend_plan<true><<<1, kThreads, seen_bytes(p), st>>>(p, seq, add, n, ws, status);
     } else {
-        scan_refs<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+        scan_refs<<<ws.n_chunks, 256, 0, st>>>(p, ws);
         extend_plan<false><<<1, kThreads, seen_bytes(p), st>>>(p, seq, add, n, ws, status);
-        list_free<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+        list_free<<<ws.n_chunks, 256, 0, st>>>(p, ws);
     }
-    extend_pages<<<dim3(n, 2 * p.n_layers), 256, 0, st>>>(p, seq, add, n, ws, status);
+    extend_pages<<<dim3(n, 2 * p.n_layers), 256, 0, st>>>(p, seq, add, n, ws);
     return hipGetLastError();
 }
 
@@ -782,9 +784,9 @@ hipError_t launch_compact(const pc_pages &p, int32_t *refs_to, int32_t *table_to
     if (p.n_pages <= kSmallPool) {
         compact_plan<true><<<1, kThreads, 0, st>>>(p, ws, n_live, status);
     } else {
-        scan_refs<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+        scan_refs<<<ws.n_chunks, 256, 0, st>>>(p, ws);
         compact_plan<false><<<1, kThreads, 0, st>>>(p, ws, n_live, status);
-        list_moves<<<ws.n_chunks, 256, 0, st>>>(p, ws, status);
+        list_moves<<<ws.n_chunks, 256, 0, st>>>(p, ws);
     }
     compact_pages<<<2048, 256, 0, st>>>(p, refs_to, table_to, ws, status);
     return hipGetLastError();

@@ -224,6 +224,38 @@ def test_groups_in_a_captured_graph():
         assert all(torch.equal(a, b) for a, b in zip(g, eager))
 
 
+def test_the_largest_batches_in_captured_graphs():
+    """More LDS than a kernel has without asking: 4,096 requests grouped, 3,000 planned and attended to."""
+    keys = torch.randint(0, 900, (4096 * 2,), device=DEV)
+    off = torch.arange(0, 4096 * 2 + 1, 2, dtype=torch.int64, device=DEV)
+    R, pages = 3000, 3000
+    k = torch.randn(1, pages, 1, 16, 64, device=DEV).to(torch.bfloat16)
+    v = torch.randn(1, pages, 1, 16, 64, device=DEV).to(torch.bfloat16)
+    table = torch.randperm(pages, device=DEV).int().reshape(R, 1).contiguous()
+    length = torch.randint(1, 17, (R,), device=DEV).int()
+    pool = dv.PagePool(k, v, table=table, length=length)
+    q = torch.randn(R, 2, 64, device=DEV).to(torch.bfloat16)
+    seq, q_off = torch.arange(R, device=DEV).int(), torch.arange(R + 1, device=DEV).int()
+    b, out = dv.PrefixBatch(pool, R, R, 2), torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        g = dv.prefix_groups(keys, off, 1)
+        b.plan(seq, q_off)
+        b.attend(0, q, out)
+    for _ in range(3):
+        keys.random_(0, 900)
+        q.normal_()
+        length.random_(1, 17)
+        graph.replay()
+        eager = dv.prefix_groups(keys, off, 1)
+        assert all(torch.equal(x, y) for x, y in zip(g, eager)) and int(g.status) == 0 and int(pool.status) == 0
+        kk, vv = k[0, table[:, 0].long(), 0].double(), v[0, table[:, 0].long(), 0].double()
+        s = torch.matmul(q.double(), kk.transpose(1, 2).contiguous()) / 8
+        w = torch.softmax(s.masked_fill((torch.arange(16, device=DEV) >= length[:, None])[:, None], -math.inf), 2)
+        o, mag = torch.matmul(w, vv), torch.matmul(w, vv.abs())
+        assert ((out.double() - o).abs() <= 2.0 ** -8 * (mag + o.abs()) + 2.0 ** -12 * mag).all()
+
+
 def test_on_another_stream():
     """All calls on a stream that is not the current one, after work on it that they depend on."""
     st = torch.cuda.Stream()
