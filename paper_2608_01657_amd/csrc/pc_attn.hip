@@ -118,12 +118,14 @@ __device__ __forceinline__ int xcd_turns(int n) { return (n + 8 * kRun - 1) / (8
 constexpr int kPlanGroups = 16;
 
 // A group's shared tokens are read for all its members at once where the row
-// tiles that this saves, times the tokens, outweigh what the joint tiles cost:
-// partial results, written and joined.  Eight requests behind 4,096 shared
-// tokens, 8 of 32 heads' K and V, together / each by itself: 900 new tokens each
-// 462 / 409 us, 100: 70 / 69, 30: 35 / 39, 17: 23 / 26; decoding, 64 requests
-// behind 1,024 tokens 22 / 36, pairs behind 4,096 85 / 91, behind 1,024 38 / 37.
-constexpr int64_t kShareCost = 16 * kTileKv;
+// tiles that this saves, times the tokens, outweigh what it costs: the joint
+// tiles' partial results, and the members' own ones, which without it go straight
+// to the output, written and joined.  32 heads on 8 of K and V, together / each by
+// itself: eight requests behind 4,096 shared tokens with 900 new tokens each 462 /
+// 409 us, 100: 70 / 69, 17: 21 / 25; decoding, 64 requests behind 930 tokens 22 /
+// 35, 512 behind 48 tokens 76 / 59, behind 128 80 / 72, in groups of eight behind
+// 240 90 / 82, behind 480 105 / 117, pairs behind 1,300 81 / 83.
+constexpr int64_t kShareCost = 16 * kTileKv, kSplitCost = 4 * kTileKv;
 
 // A segment as the plan holds it: segment i < n_req is the own tokens of the
 // request at place i of the order, segment n_req + g group g's shared tokens.
@@ -154,7 +156,7 @@ __device__ __forceinline__ uint32_t divide(uint32_t x, uint32_t d) {
 // workgroup works all segments out by itself and writes its share of the
 // queries and items; the first one writes the rest.  128 requests with 3,000
 // items took 20 us by one workgroup, most of it to write items; by 16 they take
-// 10.
+// 9.
 template <int NT>
 __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
     const pc_pages &p = a.p;
@@ -238,7 +240,7 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
         const int64_t blocks = share[g], most = least / kBlk * kBlk;
         const int64_t tokens = blocks <= 0 ? 0 : min(most, blocks * kBlk);
         const int64_t joint = ((int64_t)(t0[goff[g + 1]] - t0[goff[g]]) * G + kWideRows - 1) / kWideRows;
-        return (separate - joint) * tokens > kShareCost * joint ? (int)tokens : 0;
+        return (separate - joint) * tokens > kShareCost * joint + kSplitCost * separate ? (int)tokens : 0;
     };
     for (int g = tid; g < n_groups; g += NT) {
         const int j0 = goff[g], j1 = goff[g + 1];
@@ -389,9 +391,9 @@ __device__ __forceinline__ int swap_v_narrow(int t) { return D == 128 ? 2 * (t &
 // 32 x 32 x 16 products), and 64 tokens of K and V at a time from LDS, where a
 // second pair of buffers fills meanwhile.  16-byte pieces of a token's row are
 // permuted in LDS (see swap_k and swap_v).  Prompts of 900 tokens behind 4,096
-// cached ones run at 790 TFLOP/s (a library's product of 8192^3, which the
-// chip's power bounds too: 1,206 to 1,380).  The matrix units are busy 38 % of the time and the
-// vector units about as long; the products left out, the same prompts take 87
+// cached ones run at 790 TFLOP/s, without the plan and the join (a library's
+// product of 8192^3, which the chip's power bounds too: 1,206 to 1,380).  The
+// matrix units are busy 38 % of the time and the vector units about as long; the products left out, the same prompts take 87
 // us in place of 140, and no single part of the weights' work more than 12 us
 // (the exponentials).  What did not help: eight waves in two teams that barriers
 // kept half a tile apart (12 % longer), a wave that weighed one half of a tile
@@ -892,7 +894,7 @@ int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_h
 hipError_t launch_attn_plan(const AttnPlanArgs &a, hipStream_t st) {
     const size_t bytes = 4 * (7 * (size_t)a.n_req + 3);
     // A barrier and a sum over 16 wavefronts cost more than what few requests have to do: with 256 / 1,024
-    // threads, one request 6.7 / 9.1 us, 64 8.7 / 11.2 us, 256 11.4 / 12.0 us, 512 15.4 / 13.1 us.
+    // threads, one request 6.1 / 7.9 us, 64 8.2 / 10.0 us, 256 10.8 / 11.1 us, 512 14.5 / 12.2 us.
     if (a.n_req <= 256) {
         attn_plan<256><<<kPlanGroups, 256, bytes, st>>>(a);
         return hipGetLastError();

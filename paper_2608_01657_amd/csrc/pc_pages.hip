@@ -184,9 +184,9 @@ __global__ __launch_bounds__(256) void scan_refs(pc_pages p, PagesWs ws) {
 
 // A pool of so many pages or fewer is scanned by the one workgroup that plans;
 // larger ones by kernels of their own before and after it.  A call that finds
-// nothing to copy, one way / the other: 512 pages 7.3 / 11.4 us (extend) and 5.6 /
-// 11.2 us (compact), 16,384 pages 10.2 / 12.6 and 12.5 / 17.0, 65,536 pages 19.4 /
-// 12.5 and 35.8 / 17.2.
+// nothing to copy, one way / the other: 512 pages 6.7 / 10.5 us (extend) and 5.5 /
+// 10.3 us (compact), 16,384 pages 9.6 / 12.1 and 12.4 / 15.9, 65,536 pages 18.3 /
+// 11.8 and 35.6 / 16.1.
 constexpr int kSmallPool = 16384;
 static_assert(kSmallPool / 64 <= kThreads, "a thread for each word");
 
@@ -742,7 +742,7 @@ static size_t seen_bytes(const pc_pages &p) { return (size_t)((p.n_seqs + 31) / 
 
 // Table entries up to which one workgroup forks or frees by itself.  A fork and
 // a free of n sequences by it / by two kernels each: 4 of 16 blocks 5.5 / 7.9 us,
-// 16 of 64 6.5 / 8.0 us, 64 of 64 15.0 / 8.3 us.
+// 16 of 64 6.6 / 8.0 us, 64 of 64 14.9 / 8.2 us.
 constexpr int64_t kFewEntries = 1024;
 
 hipError_t launch_fork(const pc_pages &p, const int32_t *parent, const int32_t *child, int32_t n, int32_t *status,
@@ -821,8 +821,8 @@ hipError_t launch_groups(const uint64_t *keys, int64_t n_keys, const int64_t *ke
         return hipGetLastError();
     };
     // No more registers to sort than requests need: with four a thread, 1,024 of them took 22 us in place
-    // of 13.  256 threads for few, whose barriers and sums cost less: 8 requests 6.4 us in place of 7.0, 256
-    // 11.2 in place of 12.2 (both kernels).
+    // of 13.  256 threads for few, whose barriers and sums cost less: 8 requests 6.4 us in place of 6.7, 256
+    // 10.7 in place of 11.6 (both kernels).
     const hipError_t e = rp <= 256    ? launch(&group_requests<256, 1>, 256)
                          : rp <= 1024 ? launch(&group_requests<1024, 1>, 1024)
                          : rp <= 2048 ? launch(&group_requests<1024, 2>, 1024)

@@ -190,6 +190,20 @@ def test_shared_prefixes(heads, kv_heads, dtype, dim):
     b.check(grouped=False)
 
 
+# the same kinds of groups behind more tokens: two that decode, four, some that see only part of the shared ones
+LONGER = [(0, 130, 5, 1), (1, 190, 33, 1), (0, 130, 16, 1), (-1, 0, 70, 1), (1, 190, 1, 1), (2, 100, 40, 1),
+          (2, 100, 1, 1), (2, 100, 15, 3), (2, 100, 90, 2), (3, 165, 0, 9), (3, 165, 0, 1), (3, 165, 33, 33),
+          (3, 165, 20, 60)]
+
+
+@pytest.mark.parametrize("heads,kv_heads", HEADS)
+@pytest.mark.parametrize("dtype,dim", [(torch.bfloat16, 128), (torch.float16, 64), (torch.bfloat16, 64)])
+def test_longer_shared_prefixes(heads, kv_heads, dtype, dim):
+    b = Batch(LONGER, heads, kv_heads, dim, dtype, seed=heads, tokens_first=heads % 3 == 0)
+    b.check()
+    b.check(causal=False)
+
+
 @pytest.mark.parametrize("members", [2, 3, 16, 17, 40])
 def test_group_sizes(members):
     """Both ways that the plan goes through a group, tiles that are not full, the rule's both sides."""
@@ -385,6 +399,13 @@ def test_a_plan_for_thousands_of_requests():
     b = Batch(rows, 2, 1, 64, torch.float16)
     b.check()
     b.check(grouped=False)
+
+
+def test_a_plan_for_thousands_of_requests_that_share_more():
+    """The same, behind prefixes long enough to be read once for all: 300 pairs, 1,300 requests together."""
+    rows = [((i // 2, 100, 1 + i % 3, 1) if i < 600 else (600, 24, 1 + i % 3, 1) if i < 1900 else (-1, 0, 1 + i % 3, 1))
+            for i in range(2200)]
+    Batch(rows, 2, 1, 64, torch.float16).check()
 
 
 def test_arguments_that_python_refuses():
