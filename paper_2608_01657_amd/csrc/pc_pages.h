@@ -82,6 +82,7 @@ struct AttnHead {
 constexpr int32_t kPlanned = 0x70634174;
 struct AttnWs {
     AttnHead *head;         // 256 bytes, with kZeroOffset bytes of zeros from there on
+    int32_t *next;          // [kXcds][kNextStep]: the first of each, items of the wide list that this XCD has taken
     int32_t *tok;           // [n_tokens] query row of the query at this place of the order
     int32_t *lim;           // [n_tokens] it sees the tokens before this one
     AttnRow *row;           // [n_tokens]
@@ -92,6 +93,8 @@ struct AttnWs {
     int64_t rows;
 };
 constexpr int kZeroOffset = 128;
+constexpr int kWideSlots = 512;      // workgroups of the items' kernel, two to a CU
+constexpr int kXcds = 8, kNextStep = 32;     // a cache line to a counter
 // Bytes of the workspace (< 0: more than 2^31 - 1 partial rows).
 int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, char *base,
                 AttnWs *ws);

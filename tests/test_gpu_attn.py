@@ -408,6 +408,44 @@ def test_a_plan_for_thousands_of_requests_that_share_more():
     Batch(rows, 2, 1, 64, torch.float16).check()
 
 
+# prompts of many lengths: more tiles of more than 16 rows than there are workgroups; beside them single tokens
+PACKED = [(-1, 0, 40 + 61 * i % 300, 17 + 7 * i % 24) for i in range(70)]
+MIXED = PACKED[:40] + [(i % 3, 40, 1 + 9 * i % 50, 1) for i in range(30)] + [(3, 120, 30, 30), (3, 120, 19, 19)]
+
+
+@pytest.mark.parametrize("rows", [PACKED, MIXED], ids=["packed", "mixed"])
+@pytest.mark.parametrize("dim,dtype,heads,kv_heads", [(64, torch.bfloat16, 16, 16), (128, torch.float16, 27, 9)])
+def test_more_items_than_workgroups(rows, dim, dtype, heads, kv_heads):
+    """Workgroups that take one after another, call after call and in a graph's replays: each item once."""
+    b = Batch(rows, heads, kv_heads, dim, dtype)
+    first, _ = b.check()
+    b.check(grouped=False)
+    batch = dv.PrefixBatch(b.pool, len(rows), b.q.shape[0], heads)
+    q = b.q.to(DEV)
+    batch.plan(b.seq.to(DEV), b.q_off.to(DEV), *b.groups())
+    for _ in range(4):
+        out = torch.full_like(q, math.nan)
+        batch.attend(1, q, out)
+        assert torch.equal(out, first)
+    out.fill_(math.nan)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        batch.attend(1, q, out)
+        batch.attend(1, q, out)
+    for _ in range(4):
+        out.fill_(math.nan)
+        graph.replay()
+        assert torch.equal(out, first)
+        assert torch.equal(batch.attend(1, q), first)
+
+
+def test_the_largest_batch():
+    rows = [(-1 if i % 7 else i // 700, 3 if i % 7 == 0 else 0, 1 + i % 5, 1 + (i % 900 == 0) * (i % 5))
+            for i in range(4096)]
+    b = Batch(rows, 2, 1, 64, torch.bfloat16)
+    b.check()
+
+
 def test_arguments_that_python_refuses():
     b = Batch(DECODE, 8, 2, 64, torch.bfloat16)
     pool = b.upload()
