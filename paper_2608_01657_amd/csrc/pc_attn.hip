@@ -321,9 +321,12 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
         if (i < n_seg) ws.parts[i < n_groups ? R + i : i - n_groups] = AttnParts{x.part, direct ? -1 : chunks};
         __syncthreads();
         const int n_items = all[0], n_here = min(n_seg - i0, NT);
-        if (all[1] > kWideSlots) {
-            // segments of long items first, so that short ones end the list (32 prompts of 300 tokens behind
-            // 3,000: 245 us in place of 277)
+        // segments of long items first, so that short ones end the list (32 prompts of 300 tokens behind 3,000:
+        // 245 us in place of 277); where each workgroup has at most one, and there are no others, the second
+        // half of the workgroups, on the same CUs as the first, the other way round (one prompt of 2,000: 60 in
+        // place of 63, eight of 900 behind 4,096 145 in place of 150)
+        const bool pairs = n_seg <= NT && all[1] == all[0] && all[1] > kWideSlots / 2 && all[1] <= kWideSlots;
+        if (pairs || all[1] > kWideSlots) {
             int before = n_wide;
             for (int k = 0; k < n_here; ++k) {
                 const Segment &y = seg[k];
@@ -340,9 +343,14 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
             const uint32_t off = u - first_item[k], rest = divide(off, Hk), head = off - rest * Hk;
             const uint32_t back = divide(rest, y.chunks), c = rest - back * y.chunks, tile = y.tiles - 1 - back;
             const int b = y.kv0 + (int)c * y.per;
-            AttnItem *to = y.first >= 0 ? ws.wide + y.first : ws.narrow + (-1 - y.first);
-            to[off] = AttnItem{y.t0, y.n_tok, b, min(b + y.per, y.kv1), y.seq, (int32_t)(head | tile << 8),
-                               y.part < 0 ? -1 : y.part + (int)c * y.n_tok * a.n_heads, 0};
+            int to = (y.first >= 0 ? y.first : -1 - y.first) + (int)off;
+            if (pairs) {
+                const int half = kWideSlots / 2 / kXcds, turn = to / kXcds, turns = all[1] / kXcds;
+                if (turn >= half && turn < turns) to += (half + turns - 1 - 2 * turn) * kXcds;
+            }
+            (y.first >= 0 ? ws.wide : ws.narrow)[to] =
+                AttnItem{y.t0, y.n_tok, b, min(b + y.per, y.kv1), y.seq, (int32_t)(head | tile << 8),
+                         y.part < 0 ? -1 : y.part + (int)c * y.n_tok * a.n_heads, 0};
         }
         n_wide += all[1];
         n_narrow += all[0] - all[1];

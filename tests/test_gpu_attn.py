@@ -408,14 +408,15 @@ def test_a_plan_for_thousands_of_requests_that_share_more():
     Batch(rows, 2, 1, 64, torch.float16).check()
 
 
-# prompts of many lengths: more tiles of more than 16 rows than there are workgroups; beside them single tokens
+# prompts of many lengths: more tiles of more than 16 rows than there are workgroups, or up to two to a CU;
+# beside them single tokens
 PACKED = [(-1, 0, 40 + 61 * i % 300, 17 + 7 * i % 24) for i in range(70)]
 MIXED = PACKED[:40] + [(i % 3, 40, 1 + 9 * i % 50, 1) for i in range(30)] + [(3, 120, 30, 30), (3, 120, 19, 19)]
 
 
-@pytest.mark.parametrize("rows", [PACKED, MIXED], ids=["packed", "mixed"])
+@pytest.mark.parametrize("rows", [PACKED, PACKED[:30], MIXED], ids=["packed", "pairs", "mixed"])
 @pytest.mark.parametrize("dim,dtype,heads,kv_heads", [(64, torch.bfloat16, 16, 16), (128, torch.float16, 27, 9)])
-def test_more_items_than_workgroups(rows, dim, dtype, heads, kv_heads):
+def test_many_items_of_many_lengths(rows, dim, dtype, heads, kv_heads):
     """Workgroups that take one after another, call after call and in a graph's replays: each item once."""
     b = Batch(rows, heads, kv_heads, dim, dtype)
     first, _ = b.check()
