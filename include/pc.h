@@ -418,7 +418,7 @@ int32_t pc_prefix_groups(const uint64_t *d_keys, int64_t n_keys, const int64_t *
  * zero times infinity or NaN is NaN.
  *   d_workspace   pc_attn_workspace_bytes() bytes, 256-byte aligned; it holds the
  *                 plan from pc_attn_plan until the last pc_attn of that plan
- *                 is done. */
+ *                 is done, and their partial results: they must not overlap. */
 int64_t pc_attn_workspace_bytes(const pc_pages *pages, int32_t n_req, int64_t n_tokens, int32_t n_heads);
 
 int32_t pc_attn_plan(const pc_pages *pages, const int32_t *d_seq, const int32_t *d_q_off, int32_t n_req,
