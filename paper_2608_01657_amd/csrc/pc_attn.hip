@@ -641,14 +641,16 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
     load(it.kv0);
     const int tok = col / a.group, hq = head * a.group + col - tok * a.group;
     const bool active = tok < it.n_tok;
-    const int lim = active ? min(a.ws.lim[it.t0 + tok], it.kv1) : 0;
-    const int64_t q_row = active ? a.ws.tok[it.t0 + tok] : 0;
+    // a row behind the last reads the last query, and sees nothing
+    const int at_tok = it.t0 + min(tok, it.n_tok - 1);
+    const int lim = active ? min(a.ws.lim[at_tok], it.kv1) : 0;
+    const int64_t q_row = a.ws.tok[at_tok];
     s16x8 qf[kSteps];
     {
         const uint16_t *q = static_cast<const uint16_t *>(a.q) + q_row * a.q_token + hq * a.q_head + quarter * 8;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
-            qf[s] = active ? *reinterpret_cast<const s16x8 *>(q + 32 * s) : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+            qf[s] = *reinterpret_cast<const s16x8 *>(q + 32 * s);
     }
     f32x4 o[kDb];
 #pragma unroll
@@ -760,7 +762,8 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
 // ones.  One prompt of 8,192 tokens takes 552 us in place of 800 with turns fixed
 // beforehand, one of 20,000 for 6 heads on one of K and V 587 us in place of 757,
 // 32 of 300 behind 3,000 cached ones 245 in place of 275.  Where there are no more
-// items than workgroups, nothing is taken.  The join leaves the counters at 0.
+// items than workgroups (with narrow ones beside them: than half of these), nothing is
+// taken.  The join leaves the counters at 0.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attn_items(AttnArgs a) {
     __shared__ __align__(1024) uint16_t lds[4 * kTileKv * D];
