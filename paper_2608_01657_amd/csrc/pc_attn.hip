@@ -885,11 +885,12 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a) {
 template <typename T, int D>
 hipError_t launch(const AttnArgs &a, hipStream_t st) {
     attn_items<T, D><<<kWideSlots, 256, 0, st>>>(a);     // two workgroups to a CU
-    // A wave to a row where that does no more than fill the chip (2,700 rows of up to 36 parts: 10 us, by
-    // four rows to a wave 17 us); where there are many rows, mostly of two parts, four rows to a wave have
-    // more loads in flight (65,000 rows: 18 us, by one 38 us).
+    // A wave to a row for up to four a SIMD: those of few queries have many parts, and a wave by itself reads 16
+    // at a time.  More rows have mostly two or three parts, and with four rows to a wave more loads in flight.
+    // The whole attention by one / by four: 128 rows of four requests of 60,000 tokens 81 / 89 us, 2,700 rows 29 /
+    // 31, 4,096 62.5 / 62.7, 9,400 39 / 32, 32,000 169 / 169.
     const int64_t rows = a.n_tokens * a.n_heads, waves = a.n_tokens * ((a.n_heads + 3) / 4);
-    if (rows <= 16384) attn_join<T, D, 1><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a);
+    if (rows <= 4096) attn_join<T, D, 1><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a);
     else attn_join<T, D, 4><<<(uint32_t)((waves + 3) / 4), 256, 0, st>>>(a);
     return hipGetLastError();
 }
