@@ -16,6 +16,8 @@
 // of the second product as it lies, once the order of the tokens inside a
 // matrix instruction's k is taken to be the order in which the first product
 // leaves them.  V^T comes from row-major V by the transposing LDS read.
+#include <type_traits>
+
 #include "pc_pages.h"
 #include "pc_wave.h"
 
@@ -802,10 +804,12 @@ __global__ __launch_bounds__(256, 2) void attn_items(AttnArgs a) {
 // ------------------------------------------------------------------ join
 
 // A wave for kHeads heads of a query.  A lane weighs one part of one head, 64 /
-// kHeads parts at a time; the parts' values follow with 16 loads in flight.
+// kHeads parts at a time; the parts' values follow with 16 loads in flight, the
+// last few parts' with fewer (up to 7 % of short attentions' time: most rows
+// have two or three parts).
 template <typename T, int D, int kHeads>
 __global__ __launch_bounds__(256) void attn_join(AttnArgs a) {
-    constexpr int kParts = 64 / kHeads, kFly = 16 / kHeads, kPer = D / 64;
+    constexpr int kParts = 64 / kHeads, kFly = 16 / kHeads, kPer = D / 64, kTail = kFly < 8 ? 2 : 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per_query = (a.n_heads + kHeads - 1) / kHeads;
     if (blockIdx.x == 0 && threadIdx.x < kXcds && planned(a)) a.ws.next[threadIdx.x * kNextStep] = 0;
@@ -848,10 +852,11 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a) {
             for (int e = 0; e < kPer; ++e) o[h][e] *= fh;
         }
         const int m = min(n - c0, kParts);
-        for (int k0 = 0; k0 < m; k0 += kFly) {
-            float x[kFly][kHeads][kPer];
+        auto add = [&](auto count, int k0) {
+            constexpr int kCount = decltype(count)::value;
+            float x[kCount][kHeads][kPer];
 #pragma unroll
-            for (int k = 0; k < kFly; ++k) {
+            for (int k = 0; k < kCount; ++k) {
                 const float *from = a.ws.o + row(c0 + min(k0 + k, m - 1)) * D + kPer * lane;
 #pragma unroll
                 for (int h = 0; h < kHeads; ++h)
@@ -859,7 +864,7 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a) {
                     for (int e = 0; e < kPer; ++e) x[k][h][e] = from[min(h, heads - 1) * D + e];
             }
 #pragma unroll
-            for (int k = 0; k < kFly; ++k)
+            for (int k = 0; k < kCount; ++k)
 #pragma unroll
                 for (int h = 0; h < kHeads; ++h) {
                     // a part without tokens has no values, and the weight 0
@@ -867,7 +872,10 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a) {
 #pragma unroll
                     for (int e = 0; e < kPer; ++e) o[h][e] += wk == 0.f ? 0.f : wk * x[k][h][e];
                 }
-        }
+        };
+        int k0 = 0;
+        for (; k0 + kFly <= m; k0 += kFly) add(std::integral_constant<int, kFly>(), k0);
+        for (; k0 < m; k0 += kTail) add(std::integral_constant<int, kTail>(), k0);
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const float joined = sum == 0.f ? kNegInf : (top + log2_of(sum)) * kLn2;
@@ -887,8 +895,8 @@ hipError_t launch(const AttnArgs &a, hipStream_t st) {
     attn_items<T, D><<<kWideSlots, 256, 0, st>>>(a);     // two workgroups to a CU
     // A wave to a row for up to four a SIMD: those of few queries have many parts, and a wave by itself reads 16
     // at a time.  More rows have mostly two or three parts, and with four rows to a wave more loads in flight.
-    // The whole attention by one / by four: 128 rows of four requests of 60,000 tokens 81 / 89 us, 2,700 rows 29 /
-    // 31, 4,096 62.5 / 62.7, 9,400 39 / 32, 32,000 169 / 169.
+    // The whole attention by one / by four: 128 rows of four requests of 60,000 tokens 80 / 89 us, 2,700 rows 29 /
+    // 31, 4,096 62.6 / 62.5, 9,400 34 / 32, 32,000 169 / 169.
     const int64_t rows = a.n_tokens * a.n_heads, waves = a.n_tokens * ((a.n_heads + 3) / 4);
     if (rows <= 4096) attn_join<T, D, 1><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a);
     else attn_join<T, D, 4><<<(uint32_t)((waves + 3) / 4), 256, 0, st>>>(a);
