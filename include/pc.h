@@ -411,8 +411,9 @@ int32_t pc_prefix_groups(const uint64_t *d_keys, int64_t n_keys, const int64_t *
  * if that is sooner done), each request's own tokens by itself, and long ranges in
  * several parts; the results are joined by their sums of exponentials.  Scores, sums and joined
  * values are in 32 bits; the weights are rounded to the pool's type before
- * the product with V, where a KV head has up to 16 rows in a request (a few
- * decoding queries) to twice its bits.  Results do not depend on timing.
+ * the product with V, those of a request with up to 16 rows a KV head (a few
+ * decoding queries) to twice its bits, over shared tokens as over its own.  Results
+ * do not depend on timing.
  * K of a token that a query does not see, and K and V behind the length, may
  * hold anything.  V of the tokens within the length is finite: a weight of
  * zero times infinity or NaN is NaN.

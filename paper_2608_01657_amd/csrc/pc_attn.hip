@@ -350,9 +350,18 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
                 const int half = kWideSlots / 2 / kXcds, turn = to / kXcds, turns = all[1] / kXcds;
                 if (turn >= half && turn < turns) to += (half + turns - 1 - 2 * turn) * kXcds;
             }
+            // a wide tile with a row of a request that would be narrow by itself; only shared tokens have such tiles,
+            // and one without has fewer than ten requests
+            int exact = 0;
+            if (y.first >= 0 && i0 + k < n_groups) {
+                const int t_first = y.t0 + (int)divide(tile * kWideRows, G),
+                          t_last = y.t0 + min(y.n_tok - 1, (int)divide(tile * kWideRows + kWideRows - 1, G));
+                for (int j = last_at(t0, R, t_first); !exact && j < R && t0[j] <= t_last; ++j)
+                    exact = t0[j + 1] > t0[j] && (t0[j + 1] - t0[j]) <= kNarrowRows / G;
+            }
             (y.first >= 0 ? ws.wide : ws.narrow)[to] =
                 AttnItem{y.t0, y.n_tok, b, min(b + y.per, y.kv1), y.seq, (int32_t)(head | tile << 8),
-                         y.part < 0 ? -1 : y.part + (int)c * y.n_tok * a.n_heads, 0};
+                         y.part < 0 ? -1 : y.part + (int)c * y.n_tok * a.n_heads, exact};
         }
         n_wide += all[1];
         n_narrow += all[0] - all[1];
@@ -412,7 +421,13 @@ __device__ __forceinline__ int swap_v_narrow(int t) { return D == 128 ? 2 * (t &
 // between the products of the others (1 % longer), tiles of 32 tokens (6 %),
 // wave priorities (the same).  Products of four independent sums in turn, their
 // reads issued four products ahead, save 2 %.
-template <typename T, int D>
+//
+// kWeights: in how many pieces the weights go into the second product.  One, rounded to the type of K and V, for
+// prompts, two, exact to twice its bits, where a row is of a request with few (a token that decodes has the same
+// precision whoever shares its prefix).  Two everywhere would take eight prompts of 900 behind 4,096 from 137 to 177 us
+// and one of 8,192 from 281 to 362, for errors of 1.7e-3 in place of 2.3e-3 (bf16, whose results round by 1.7e-3);
+// where the rows decode, reading the tokens hides them: 128 requests behind 8,192 tokens take 64.3 us in place of 62.2.
+template <typename T, int D, int kWeights>
 __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, uint16_t *lds, int *lds_lim, int *queue,
                                           int &next) {
     constexpr int kPieces = D / 8, kSteps = D / 16, kDb = D / 32, kBuf = kTileKv * D;   // K, K, V, V
@@ -535,7 +550,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
             m = now;
         }
         const float use = m == kNegInf ? 0.f : m;
-        s16x8 pf[4];
+        s16x8 pf[4], rest[4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -549,6 +564,11 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
 #pragma unroll
                 for (int y = 0; y < 4; ++y) w.u[y] = T::pack(s[h][8 * x + 2 * y], s[h][8 * x + 2 * y + 1]);
                 pf[2 * h + x] = w.v;
+                if (kWeights == 1) continue;
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    w.u[y] = T::pack_rest(s[h][8 * x + 2 * y], s[h][8 * x + 2 * y + 1], w.u[y]);
+                rest[2 * h + x] = w.v;
             }
         }
         const int quad = (lane >> 2) & 3, g16 = (lane >> 4) & 1;
@@ -559,16 +579,18 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
             for (int i = 0; i < kDb; ++i) {
                 const int piece = (4 * i + 2 * g16 + ((lane & 3) >> 1)) ^ swap_v<D>(vt);
                 const uint16_t *v = lv + vt * D + piece * 8 + (lane & 1) * 4;
-                o[i] = T::mma32(join(read_tr(v + st * 16 * D), read_tr(v + (st * 16 + 8) * D)), pf[st], o[i]);
+                const s16x8 v8 = join(read_tr(v + st * 16 * D), read_tr(v + (st * 16 + 8) * D));
+                o[i] = T::mma32(v8, pf[st], o[i]);
+                if (kWeights == 2) o[i] = T::mma32(v8, rest[st], o[i]);
             }
         // four products' reads ahead of the first one
         __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
 #pragma unroll
         for (int i = 0; i < 4 * kDb - 4; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x008, kWeights, 1);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
+        __builtin_amdgcn_sched_group_barrier(0x008, 4 * kWeights, 1);
     }
     // no sooner: who takes an item long before it can begin keeps it from others.  Looked at behind the stores.
     if (queue && threadIdx.x == 0) next = atomicAdd(queue, 1);
@@ -781,8 +803,11 @@ __global__ __launch_bounds__(256, 2) void attn_items(AttnArgs a) {
             int turn = blockIdx.x / kXcds, next = 0;
             bool have = turn < given && turn * kXcds + xcd < n_wide;
             while (have || queue) {
-                if (have) wide_item<T, D>(a, a.ws.wide[turn * kXcds + xcd], lds, lds_lim, queue, next);
-                else if (threadIdx.x == 0) next = atomicAdd(queue, 1);
+                if (have) {
+                    const AttnItem it = a.ws.wide[turn * kXcds + xcd];
+                    if (it.exact) wide_item<T, D, 2>(a, it, lds, lds_lim, queue, next);
+                    else wide_item<T, D, 1>(a, it, lds, lds_lim, queue, next);
+                } else if (threadIdx.x == 0) next = atomicAdd(queue, 1);
                 if (!queue) break;
                 __syncthreads();
                 if (threadIdx.x == 0) lds_next = given + next;

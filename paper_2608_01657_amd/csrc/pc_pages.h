@@ -63,7 +63,7 @@ struct AttnItem {
     int32_t seq;            // whose table row holds the pages
     int32_t head_tile;      // KV head | tile << 8
     int32_t part;           // partial row of (first query, head 0); -1: straight to the output
-    int32_t pad;
+    int32_t exact;          // whether its weights go in two pieces (wide ones; narrow ones always do)
 };
 // Where a segment's partial results are: their first row, and how many parts
 // each query has (-1: they go straight to the output).
