@@ -33,7 +33,10 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+// kLift: the weights are multiplied by 2^kLift on their way to the second product (and their sum with them), so that
+// small ones keep their bits in a type of few exponents.
 struct Bf16 {
+    static constexpr float kLift = 0.f;
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     static __device__ f32x16 mma32(s16x8 a, s16x8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
@@ -51,6 +54,9 @@ struct Bf16 {
     }
 };
 struct Fp16 {
+    // 2^8 times this stays below the largest value, and 2^-32 of the greatest weight is what gets lost, in place of
+    // 2^-25: behind a token that takes nearly all, 20,000 others may share 1/2,000
+    static constexpr float kLift = 7.f;
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     static __device__ f32x16 mma32(s16x8 a, s16x8 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
@@ -95,8 +101,8 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
 
 // The running maximum follows the scores only where they pass it by this much
-// (in powers of two): weights up to 2^8 lose nothing in any of the types, and
-// most tiles are spared the scaling of O.
+// (in powers of two): weights up to 2^8 lose nothing in any of the types (see
+// kLift), and most tiles are spared the scaling of O.
 constexpr float kSlack = 8.f;
 
 // Every load of the wave has landed in LDS.
@@ -549,7 +555,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
                 for (int r = 0; r < 16; ++r) o[i][r] *= f;
             m = now;
         }
-        const float use = m == kNegInf ? 0.f : m;
+        const float use = m == kNegInf ? 0.f : m - T::kLift;
         s16x8 pf[4], rest[4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -597,7 +603,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs &a, const AttnItem it, 
     l += __shfl_xor(l, 32);
     if (active) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const float lse = l == 0.f ? kNegInf : m + log2_of(l);
+        const float lse = l == 0.f ? kNegInf : m - T::kLift + log2_of(l);
         if (it.part < 0) {
             uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + hq * a.out_head + 4 * half;
 #pragma unroll
@@ -719,7 +725,7 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
             for (int i = 0; i < kDb; ++i) o[i] *= f;
             m = now;
         }
-        const float use = m == kNegInf ? 0.f : m;
+        const float use = m == kNegInf ? 0.f : m - T::kLift;
         union { uint32_t u[2 * kPages]; s16x8 v[kPages / 2]; } w, rest;
 #pragma unroll
         for (int h = 0; h < kPages; ++h) {
@@ -752,7 +758,7 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
     l += __shfl_xor(l, 32);
     if (active) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const float lse = l == 0.f ? kNegInf : m + log2_of(l);
+        const float lse = l == 0.f ? kNegInf : m - T::kLift + log2_of(l);
         if (it.part < 0) {
             uint16_t *to = static_cast<uint16_t *>(a.out) + q_row * a.out_token + hq * a.out_head + 4 * quarter;
 #pragma unroll

@@ -13,6 +13,7 @@ import math
 import pytest
 import torch
 
+from paper_2608_01657_amd import device as dv
 from test_gpu_attn import DEV, U, Batch
 
 pytestmark = pytest.mark.gpu
@@ -99,3 +100,31 @@ def test_the_same_answer_alone_and_in_a_group(dtype, dim):
     b = batch(rows, 8, 2, dim, dtype)
     check(b, range(40))
     check(b, range(40), grouped=False)
+
+
+@pytest.mark.parametrize("dtype,dim", [(torch.bfloat16, 64), (torch.float16, 64), (torch.float16, 128)])
+@pytest.mark.parametrize("new", [1, 40], ids=["decode", "prompt"])
+def test_many_small_weights_behind_a_great_one(new, dtype, dim):
+    """The first token takes nearly all of each row and has V = 0; 20,000 others, each with 2^-25.4 of its weight,
+    have V = 1, so that the result is their share, some 2^-11.1.  Requests enough (all of one sequence) that none is
+    split along its tokens.  Off by at most: 2^-32 of the first weight for each token (what a type of few exponents
+    loses), u for the weights, u for the result, 2^-24 (16 |s| + 4 n + 64)."""
+    R, n, score = 512, 20000 + new, 17.625      # 25.43 powers of two
+    pages = -(-n // 16)
+    k = torch.zeros(1, pages, 2, 16, dim, dtype=dtype, device=DEV)
+    v = torch.ones_like(k)
+    k[0, 0, :, 0, 0] = 1
+    v[0, 0, :, 0] = 0
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    pool = dv.PagePool(k, v, table=torch.arange(pages, dtype=torch.int32, device=DEV)[None].contiguous(), length=i32([n]))
+    q = torch.zeros(R * new, 4, dim, dtype=dtype, device=DEV)
+    q[:, :, 0] = score
+    b = dv.PrefixBatch(pool, R, R * new, 4)
+    b.plan(i32([0] * R), torch.arange(0, R * new + 1, new, dtype=torch.int32, device=DEV))
+    out = b.attend(0, q, scale=1.0).double().reshape(R, new, 4 * dim)
+    assert int(pool.status) == 0
+    seen = torch.arange(n - new, n, dtype=torch.float64, device=DEV)[:, None]     # tokens behind the first
+    o = seen * math.exp(-score) / (1 + seen * math.exp(-score))
+    u = U[dtype]
+    tol = n * 2.0 ** -32 + o * (2 * u + u * u + 2.0 ** -24 * (16 * score + 4 * n + 64))
+    assert ((out - o).abs() <= tol).all(), float((out / o - 1).abs().max())
