@@ -716,6 +716,7 @@ __global__ __launch_bounds__(256) void group_shared(const uint64_t *keys, const 
         }
         if (threadIdx.x == 0) atomicMin(&shared[g], first_off);
     }
+    __syncthreads();        // all waves have read their word: x
     if (threadIdx.x == 0) __hip_atomic_store(&order[q], i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
