@@ -383,11 +383,12 @@ int32_t pc_pages_write(const pc_pages *pages, int32_t layer, const int32_t *d_se
  *                d_group_off[n_groups] on
  *   d_shared     [n_req] leading blocks with the same keys in all requests of
  *                group g; 0 for a group of one and behind the last group
- *   d_n_groups   [1]
+ *   d_n_groups   [1]; -1 where the offsets are refused, which pc_attn_plan
+ *                refuses in its turn
  * n_req is at most PC_MAX_BATCH (else PC_EUNSUPPORTED), a request has 2^26
  * blocks at most.  d_status, written by every call and not read: PC_OK, or
- * PC_EINVAL where the offsets fall or leave [0, n_keys] (nothing else is written
- * then). */
+ * PC_EINVAL where the offsets fall or leave [0, n_keys] (only d_n_groups is
+ * written beside it then). */
 int32_t pc_prefix_groups(const uint64_t *d_keys, int64_t n_keys, const int64_t *d_key_off, int32_t n_req,
                          int32_t min_blocks, int32_t *d_order, int32_t *d_group_off, int32_t *d_shared,
                          int32_t *d_n_groups, int32_t *d_status, void *stream);

@@ -595,7 +595,10 @@ __global__ __launch_bounds__(NT) void group_requests(const uint64_t *keys, int64
         if (blocks[e] >= min_blocks) mark[i] = keys[a + min_blocks - 1];
     }
     __syncthreads();
-    if (tid == 0) *status = any_bad ? PC_EINVAL : PC_OK;
+    if (tid == 0) {
+        *status = any_bad ? PC_EINVAL : PC_OK;
+        if (any_bad) *n_groups = -1;
+    }
     if (any_bad) return;
     const uint32_t slots = 2 * Rp;
 #pragma unroll
@@ -684,11 +687,12 @@ __global__ __launch_bounds__(NT) void group_requests(const uint64_t *keys, int64
 }
 
 // A workgroup for each request: how many leading keys it has in common with
-// its group's first one.
+// its group's first one.  It goes by the number of groups, which this call alone
+// writes, and not by the status.
 __global__ __launch_bounds__(256) void group_shared(const uint64_t *keys, const int64_t *key_off, int32_t *order,
                                                     const int32_t *group_off, int32_t *shared,
-                                                    const int32_t *status) {
-    if (*status != PC_OK) return;
+                                                    const int32_t *n_groups) {
+    if (*n_groups < 0) return;
     __shared__ int first_off;
     const int q = blockIdx.x;
     const int x = order[q], g = x / PC_MAX_BATCH, i = x % PC_MAX_BATCH;
@@ -829,7 +833,7 @@ hipError_t launch_groups(const uint64_t *keys, int64_t n_keys, const int64_t *ke
                          : rp <= 2048 ? launch(&group_requests<1024, 2>, 1024)
                                       : launch(&group_requests<1024, 4>, 1024);
     if (e != hipSuccess) return e;
-    group_shared<<<n_req, 256, 0, st>>>(keys, key_off, order, group_off, shared, status);
+    group_shared<<<n_req, 256, 0, st>>>(keys, key_off, order, group_off, shared, n_groups);
     return hipGetLastError();
 }
 
