@@ -280,7 +280,9 @@ int32_t pc_get_stats(const void *d_stats, int32_t n_inst, int32_t instance,
  * otherwise.  A call that finds it set does nothing, so that calls may be
  * queued one after another (or captured) and looked at once, at the end.
  * Calls that may overlap (on other streams) have a status of their own each, or
- * may be stopped by each other's errors.  No call reads or writes outside the
+ * may be stopped by each other's errors, pc_pages_write in the middle and the others
+ * as a whole.  A call that is refused or stopped may turn a length that is out of
+ * range into another one that is.  No call reads or writes outside the
  * buffers described here, whatever the lists and tables hold.
  *
  * Every call can be captured into a HIP graph.  A workspace holds nothing

@@ -6,9 +6,9 @@
 // acts, and the second does nothing where the first set the status: a call
 // happens whole or not at all.  Counts change by integer atomics, whose order
 // does not matter; new pages go by rank among the free ones, so results do not
-// depend on timing.  Where there is a workspace, the kernels behind the check go
-// by a word in it, written by one workgroup, and not by the status, which
-// another call may set meanwhile.
+// depend on timing.  The kernels behind the check do not go by the status, which
+// another call may set meanwhile, but by a word that one workgroup of their own
+// call writes: in the workspace where there is one, else in the lengths (kGo).
 #include "pc_pages.h"
 #include "pc_wave.h"
 
@@ -92,8 +92,8 @@ __device__ bool bad_pages(const pc_pages &p, uint32_t s, int at, int step) {
     return bad;
 }
 
-__device__ void fork_one(const pc_pages &p, int64_t from, int64_t to, int at, int step) {
-    const int len = p.d_len[from], nb = blocks_of(len);
+__device__ void fork_one(const pc_pages &p, int64_t from, int64_t to, int len, int at, int step) {
+    const int nb = blocks_of(len);
     const int32_t *src = p.d_table + from * p.table_width;
     int32_t *dst = p.d_table + to * p.table_width;
     for (int i = at; i < nb; i += step) {
@@ -110,6 +110,14 @@ __device__ void free_one(const pc_pages &p, int64_t s, int len, int at, int step
     for (int i = at; i < nb; i += step) atomicSub(&p.d_refs[row[i]], 1);
 }
 
+// Beside the length of a sequence that is about to be filled or emptied, between
+// two kernels of one call.  No length that is in range has it; one out of range
+// that looks like this becomes another one out of range.
+constexpr int32_t kGo = 1 << 30;
+constexpr int32_t kNoLength = 0x7fffffff;
+
+__device__ __forceinline__ bool goes(const pc_pages &p, int32_t len) { return len >= kGo && len_ok(p, len - kGo); }
+
 // Workgroup 0 looks at the lists, the others each at one sequence's pages.
 __global__ __launch_bounds__(256) void check_lists(pc_pages p, const int32_t *seq, const int32_t *child, int32_t n,
                                                    int32_t *status) {
@@ -120,18 +128,41 @@ __global__ __launch_bounds__(256) void check_lists(pc_pages p, const int32_t *se
     if (bad) atomicExch(status, PC_EINVAL);
 }
 
-__global__ __launch_bounds__(256) void fork_pages(pc_pages p, const int32_t *parent, const int32_t *child,
-                                                  const int32_t *status) {
-    if (*status != PC_OK) return;
-    fork_one(p, parent[blockIdx.x], child[blockIdx.x], threadIdx.x, blockDim.x);
+// One workgroup reads the status once and says to all sequences whether the
+// call happens.  A launch between the other two, 1.6 us: without it every
+// workgroup, and every wave, read the status for itself, and what another call
+// set at that moment stopped some of them.
+__global__ __launch_bounds__(kThreads) void decide(pc_pages p, const int32_t *seq, const int32_t *child, int32_t n,
+                                                   const int32_t *status) {
+    __shared__ int32_t now;
+    if (threadIdx.x == 0) now = __hip_atomic_load(status, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int i0 = 0; i0 < n; i0 += kThreads) {
+        const int i = i0 + threadIdx.x;
+        const uint32_t from = i < n ? (uint32_t)seq[i] : ~0u, to = i < n && child ? (uint32_t)child[i] : from;
+        const bool in = from < (uint32_t)p.n_seqs, ends = to < (uint32_t)p.n_seqs;      // if not, the call is refused
+        const int32_t len = in ? p.d_len[from] : 0, old = ends ? p.d_len[to] : 0;
+        if (i0 == 0) __syncthreads();       // behind the loads: now
+        if (in && ends && now == PC_OK) p.d_len[to] = len | kGo;
+        else if (ends && goes(p, old)) p.d_len[to] = kNoLength;
+    }
 }
 
-__global__ __launch_bounds__(256) void free_pages(pc_pages p, const int32_t *seq, const int32_t *status) {
-    if (*status != PC_OK) return;
-    const int64_t s = seq[blockIdx.x];
-    const int len = p.d_len[s];
+__global__ __launch_bounds__(256) void fork_pages(pc_pages p, const int32_t *parent, const int32_t *child) {
+    const uint32_t c = (uint32_t)child[blockIdx.x];
+    if (c >= (uint32_t)p.n_seqs) return;
+    const int32_t len = p.d_len[c];
+    if (!goes(p, len)) return;
     __syncthreads();        // all have read it
-    free_one(p, s, len, threadIdx.x, blockDim.x);
+    fork_one(p, parent[blockIdx.x], c, len - kGo, threadIdx.x, blockDim.x);
+}
+
+__global__ __launch_bounds__(256) void free_pages(pc_pages p, const int32_t *seq) {
+    const uint32_t s = (uint32_t)seq[blockIdx.x];
+    if (s >= (uint32_t)p.n_seqs) return;
+    const int32_t len = p.d_len[s];
+    if (!goes(p, len)) return;
+    __syncthreads();        // all have read it
+    free_one(p, s, len - kGo, threadIdx.x, blockDim.x);
     if (threadIdx.x == 0) p.d_len[s] = 0;
 }
 
@@ -153,7 +184,7 @@ __global__ __launch_bounds__(kThreads) void fork_or_free_few(pc_pages p, const i
     }
     for (int i = wave; i < n; i += kThreads / 64) {
         if (child) {
-            fork_one(p, seq[i], child[i], lane, 64);
+            fork_one(p, seq[i], child[i], p.d_len[seq[i]], lane, 64);
         } else {
             const int len = p.d_len[seq[i]];
             free_one(p, seq[i], len, lane, 64);
@@ -756,7 +787,8 @@ hipError_t launch_fork(const pc_pages &p, const int32_t *parent, const int32_t *
         fork_or_free_few<<<1, kThreads, seen_bytes(p), st>>>(p, parent, child, n, status);
     } else {
         check_lists<<<n + 1, 256, seen_bytes(p), st>>>(p, parent, child, n, status);
-        fork_pages<<<n, 256, 0, st>>>(p, parent, child, status);
+        decide<<<1, kThreads, 0, st>>>(p, parent, child, n, status);
+        fork_pages<<<n, 256, 0, st>>>(p, parent, child);
     }
     return hipGetLastError();
 }
@@ -766,7 +798,8 @@ hipError_t launch_free(const pc_pages &p, const int32_t *seq, int32_t n, int32_t
         fork_or_free_few<<<1, kThreads, seen_bytes(p), st>>>(p, seq, nullptr, n, status);
     } else {
         check_lists<<<n + 1, 256, seen_bytes(p), st>>>(p, seq, nullptr, n, status);
-        free_pages<<<n, 256, 0, st>>>(p, seq, status);
+        decide<<<1, kThreads, 0, st>>>(p, seq, nullptr, n, status);
+        free_pages<<<n, 256, 0, st>>>(p, seq);
     }
     return hipGetLastError();
 }

@@ -1,0 +1,83 @@
+"""The status that calls on pages share: a call happens whole or not at all,
+whenever another one sets it."""
+import pytest
+import torch
+
+import paper_2608_01657_amd as P
+from paper_2608_01657_amd import device as dv
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def pool_of(n_seqs, width, n_pages):
+    k = torch.zeros(1, n_pages, 1, 16, 64, dtype=torch.bfloat16, device=DEV)
+    return dv.PagePool(k, k.clone(), n_seqs=n_seqs, table_width=width)
+
+
+@pytest.mark.parametrize("n,blocks", [(200, 90), (8, 300), (300, 3)])
+def test_a_status_set_meanwhile_stops_a_fork_or_a_free_whole(n, blocks):
+    """Another stream sets the status at some time or other while sequences are forked and freed: all
+    children have all pages, or none has any."""
+    pool = pool_of(2 * n, blocks, n * blocks)
+    parent, child = torch.arange(n, dtype=torch.int32, device=DEV), torch.arange(n, 2 * n, dtype=torch.int32, device=DEV)
+    pool.extend(parent, i32([16 * blocks] * n))
+    assert int(pool.status) == 0
+    pages = pool.table[:n].clone()
+    here, there = torch.cuda.Stream(), torch.cuda.Stream()
+    junk = torch.zeros(1 << 14, device=DEV)
+    happened = set()
+    torch.cuda.synchronize()
+    for step in range(120):
+        for what in ("fork", "free"):
+            with torch.cuda.stream(there):
+                for _ in range(step % 12):
+                    junk.add_(1)
+                pool.status.fill_(P.PC_EINVAL)
+            if what == "fork":
+                pool.fork(parent, child, stream=here)
+            else:
+                pool.free(child, stream=here)
+            torch.cuda.synchronize()
+            pool.status.zero_()
+            held = int((pool.length[n:] > 0).sum())
+            assert held in (0, n) and int((pool.length[n:] == 16 * blocks).sum()) == held
+            assert (pool.length[:n] == 16 * blocks).all() and torch.equal(pool.table[:n], pages)
+            assert (pool.refs == (2 if held else 1)).all()
+            if held:
+                assert torch.equal(pool.table[n:], pages)
+            happened.add((what, held))
+            if held and what == "free":     # was stopped
+                pool.free(child)
+            torch.cuda.synchronize()
+    assert ("fork", n) in happened or ("fork", 0) in happened
+
+
+@pytest.mark.parametrize("n,blocks", [(2, 3), (40, 100)])
+def test_lengths_out_of_range_stay_so(n, blocks):
+    """Refused and stopped calls leave every length that is in range, and none that is not becomes one."""
+    pool = pool_of(n, blocks, n * blocks)
+    pool.extend(torch.arange(n // 2, dtype=torch.int32, device=DEV), i32([16 * blocks] * (n // 2)))
+    refs, table = pool.refs.clone(), pool.table.clone()
+    good = pool.length.clone()
+    for bad in (-1, -2 ** 31, 16 * blocks + 1, 2 ** 30, 2 ** 30 + 16, 2 ** 30 + 16 * blocks, 2 ** 31 - 1):
+        for status in (0, P.PC_ENOPAGES):
+            for f in (lambda: pool.free(torch.arange(n, dtype=torch.int32, device=DEV)),
+                      lambda: pool.fork(torch.arange(n // 2, dtype=torch.int32, device=DEV),
+                                        torch.arange(n // 2, n, dtype=torch.int32, device=DEV))):
+                pool.length.copy_(good)
+                pool.length[n - 1] = bad
+                pool.status.fill_(status)
+                f()
+                assert int(pool.status) == (status or P.PC_EINVAL)
+                assert torch.equal(pool.length[:n - 1], good[:n - 1])
+                assert not 0 <= int(pool.length[n - 1]) <= 16 * blocks
+                assert torch.equal(pool.refs, refs) and torch.equal(pool.table, table)
+    pool.length.copy_(good)
+    pool.status.zero_()
+    pool.free(torch.arange(n, dtype=torch.int32, device=DEV))
+    assert int(pool.status) == 0 and int(pool.refs.abs().sum()) == 0 and int(pool.length.abs().sum()) == 0
