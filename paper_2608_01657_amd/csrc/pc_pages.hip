@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256) void free_pages(pc_pages p, const int32_t *seq
     if (threadIdx.x == 0) p.d_len[s] = 0;
 }
 
-// Both steps by one workgroup, a wave to a sequence (see kFewEntries).
+// Both steps by one workgroup, a wave to a sequence (see few).
 __global__ __launch_bounds__(kThreads) void fork_or_free_few(pc_pages p, const int32_t *seq, const int32_t *child,
                                                              int32_t n, int32_t *status) {
     extern __shared__ uint32_t seen[];
@@ -776,14 +776,15 @@ int64_t pages_ws(const pc_pages &p, int64_t n, char *base, PagesWs *ws) {
 
 static size_t seen_bytes(const pc_pages &p) { return (size_t)((p.n_seqs + 31) / 32) * 4; }
 
-// Table entries up to which one workgroup forks or frees by itself.  A fork and
-// a free of n sequences by it / by two kernels each: 4 of 16 blocks 5.5 / 7.9 us,
-// 16 of 64 6.6 / 8.0 us, 64 of 64 14.9 / 8.2 us.
-constexpr int64_t kFewEntries = 1024;
+// Whether one workgroup forks or frees by itself, a wave to a sequence.  A fork and a free of n sequences of so many
+// blocks by it / by three kernels each: 1 of 14 6.0 / 10.3 us, 16 of 64 6.9 / 11.5, 16 of 200 9.5 / 12.1, 16 of 600
+// 15.3 / 13.5, 1 of 4,000 52 / 24; with two to a wave 32 of 32 9.0 / 11.6, 32 of 128 11.7 / 11.6, with four 64 of 14
+// 15.9 / 11.8.  The host knows how wide the table is, not how much of it is in use.
+static bool few(const pc_pages &p, int32_t n) { return n <= 16 ? p.table_width <= 640 : n <= 32 && p.table_width <= 128; }
 
 hipError_t launch_fork(const pc_pages &p, const int32_t *parent, const int32_t *child, int32_t n, int32_t *status,
                        hipStream_t st) {
-    if ((int64_t)n * p.table_width <= kFewEntries) {
+    if (few(p, n)) {
         fork_or_free_few<<<1, kThreads, seen_bytes(p), st>>>(p, parent, child, n, status);
     } else {
         check_lists<<<n + 1, 256, seen_bytes(p), st>>>(p, parent, child, n, status);
@@ -794,7 +795,7 @@ hipError_t launch_fork(const pc_pages &p, const int32_t *parent, const int32_t *
 }
 
 hipError_t launch_free(const pc_pages &p, const int32_t *seq, int32_t n, int32_t *status, hipStream_t st) {
-    if ((int64_t)n * p.table_width <= kFewEntries) {
+    if (few(p, n)) {
         fork_or_free_few<<<1, kThreads, seen_bytes(p), st>>>(p, seq, nullptr, n, status);
     } else {
         check_lists<<<n + 1, 256, seen_bytes(p), st>>>(p, seq, nullptr, n, status);
