@@ -296,6 +296,7 @@ enum { PC_HEADS_FIRST = 0,            /* a page is [n_kv_heads][16][head_dim]   
 #define PC_MAX_SEQS 262144            /* sequences of a pool                           */
 #define PC_MAX_POOL_PAGES (1 << 27)
 #define PC_MAX_BATCH 4096             /* requests of one batch, sequences that grow at once */
+#define PC_ATTN_HEAD_BYTES 256        /* of an attention's workspace, zeroed by the caller once */
 
 typedef struct {
     void *d_k, *d_v;                  /* page 0 of layer 0, 16-byte aligned            */
@@ -422,7 +423,10 @@ int32_t pc_prefix_groups(const uint64_t *d_keys, int64_t n_keys, const int64_t *
  * zero times infinity or NaN is NaN.
  *   d_workspace   pc_attn_workspace_bytes() bytes, 256-byte aligned; it holds the
  *                 plan from pc_attn_plan until the last pc_attn of that plan
- *                 is done, and their partial results: they must not overlap. */
+ *                 is done, and their partial results: they must not overlap.
+ *                 Its first PC_ATTN_HEAD_BYTES are zeroed by the caller when the
+ *                 memory becomes a workspace: a plan that it held before would
+ *                 be taken for this one's. */
 int64_t pc_attn_workspace_bytes(const pc_pages *pages, int32_t n_req, int64_t n_tokens, int32_t n_heads);
 
 int32_t pc_attn_plan(const pc_pages *pages, const int32_t *d_seq, const int32_t *d_q_off, int32_t n_req,

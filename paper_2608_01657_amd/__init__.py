@@ -38,6 +38,7 @@ PC_LAYOUT_LDS, PC_LAYOUT_HYBRID, PC_LAYOUT_WS = 0, 1, 2
 PC_BF16, PC_FP16 = 0, 1
 PC_HEADS_FIRST, PC_TOKENS_FIRST = 0, 1
 PC_MAX_SEQS, PC_MAX_POOL_PAGES, PC_MAX_BATCH = 262144, 1 << 27, 4096
+PC_ATTN_HEAD_BYTES = 256
 LAYOUT_NAMES = {PC_LAYOUT_LDS: "lds", PC_LAYOUT_HYBRID: "hybrid", PC_LAYOUT_WS: "workspace"}
 
 GROUP_FIELDS = ["requests", "probes", "hits", "misses", "charged", "evicted_owned",

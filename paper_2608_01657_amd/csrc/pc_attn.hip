@@ -950,7 +950,8 @@ int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_h
     if (rows > 0x7fffffff || wide > 0x7fffffff) return -1;
     int64_t o = 0;
     auto take = [&](int64_t bytes) { const int64_t at = o; o += up(bytes); return at; };
-    const int64_t head = take(256), next = take(4 * kXcds * kNextStep), tok = take(4 * n_tokens), lim = take(4 * n_tokens), row = take(n_tokens * (int64_t)sizeof(AttnRow)),
+    static_assert(PC_ATTN_HEAD_BYTES == 256 && sizeof(AttnHead) <= kZeroOffset, "the head, and the zeros behind it");
+    const int64_t head = take(PC_ATTN_HEAD_BYTES), next = take(4 * kXcds * kNextStep), tok = take(4 * n_tokens), lim = take(4 * n_tokens), row = take(n_tokens * (int64_t)sizeof(AttnRow)),
                   parts = take(2LL * n_req * (int64_t)sizeof(AttnParts)),
                   w = take(wide * (int64_t)sizeof(AttnItem)), nr = take(narrow * (int64_t)sizeof(AttnItem)),
                   po = take(rows * head_dim * 4), pl = take(rows * 4);

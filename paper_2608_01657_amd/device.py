@@ -18,7 +18,7 @@ from . import (make_instance_desc, make_pages, make_rows, phase_counters, make_t
                pc_attn_workspace_bytes, pc_block_offsets, pc_get_stats, pc_hash_blocks, pc_pages_compact,
                pc_pages_extend, pc_pages_fork, pc_pages_free, pc_pages_workspace_bytes, pc_pages_write,
                pc_prefix_groups, pc_replay_batch, pc_replay_route_offset, pc_replay_workspace_bytes, pc_replay_workspace_min_bytes,
-               stats_to_dicts, PC_BLOCK_TOKENS, PC_ROUTE_GENERAL, PC_STATS_RECORD_BYTES)
+               stats_to_dicts, PC_ATTN_HEAD_BYTES, PC_BLOCK_TOKENS, PC_ROUTE_GENERAL, PC_STATS_RECORD_BYTES)
 
 
 @dataclass
@@ -419,6 +419,7 @@ class PrefixBatch:
         self.pool, self.n_req, self.n_tokens, self.n_heads = pool, n_req, n_tokens, n_heads
         n = pc_attn_workspace_bytes(pool.desc, n_req, n_tokens, n_heads)
         self.workspace = torch.empty(n, dtype=torch.uint8, device=pool.device)
+        self.workspace[:PC_ATTN_HEAD_BYTES].zero_()     # memory of a batch that is gone may hold its plan
 
     def plan(self, seq, q_off, order=None, group_off=None, shared=None, n_groups=None, causal: bool = True,
              stream=None):
