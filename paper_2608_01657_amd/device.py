@@ -273,24 +273,47 @@ def _list(x, dev, what, dtype=torch.int32):
 
 
 @contextlib.contextmanager
-def _other(dev, stream):
-    """`dev` is the current device, and `stream` the one that new tensors belong to."""
+def _other(dev, stream, owner, tensors):
+    """`dev` is the current device, and `stream` the one that new tensors belong to.  What a call uses there
+    is not handed out again before the stream is done with it: its arguments, and the owner's tensors.  (Of a
+    raw handle nobody says how long it lives, so there the caller keeps them; a captured graph's user does so
+    anyway.)"""
     with torch.cuda.device(dev):
-        if isinstance(stream, torch.cuda.Stream):
-            with torch.cuda.stream(stream):
-                yield
-        else:
+        if stream is None:
+            yield
+            return
+        known = isinstance(stream, torch.cuda.Stream)
+        if not known:
+            stream = torch.cuda.ExternalStream(getattr(stream, "cuda_stream", stream), device=dev)
+        with torch.cuda.stream(stream):
+            if known and not torch.cuda.is_current_stream_capturing():
+                if owner is not None:
+                    owner._used_on(stream)
+                for x in tensors:
+                    if x is not None and x.is_cuda:     # others are refused by the call
+                        x.record_stream(stream)
             yield
 
 
 _here = contextlib.nullcontext()
 
 
-def _on(dev, stream):
-    return _here if stream is None and torch.cuda.current_device() == dev.index else _other(dev, stream)
+def _on(dev, stream, owner, *tensors):
+    return (_here if stream is None and torch.cuda.current_device() == dev.index
+            else _other(dev, stream, owner, tensors))
 
 
-class PagePool:
+class _Owner:
+    """Tensors that belong to an object, kept for the streams that it is used on."""
+
+    def _used_on(self, stream):
+        if stream.cuda_stream not in self._streams:
+            self._streams.add(stream.cuda_stream)
+            for x in self._tensors():
+                x.record_stream(stream)
+
+
+class PagePool(_Owner):
     """The pages of a KV cache and the sequences that hold them: 16 tokens a
     page, K and V [layers, pages, heads, 16, dim], or [layers, pages, 16,
     heads, dim] with tokens_first; the layers and pages may be strided, a page
@@ -300,7 +323,10 @@ class PagePool:
     `refs` [pages] (holders), all int32; made empty unless given.  `status`
     collects what the calls find wrong on the device (PC_EINVAL, PC_ENOPAGES):
     once it is set, further calls do nothing until it is zeroed.  Every call
-    is asynchronous and can be captured into a graph."""
+    is asynchronous and can be captured into a graph.
+
+    A call goes to the current stream, or to the one given: a torch.cuda.Stream,
+    or a raw handle, whose calls' tensors the caller keeps until they are done."""
 
     def __init__(self, k, v, n_seqs: Optional[int] = None, table_width: Optional[int] = None, table=None, length=None,
                  refs=None, tokens_first: bool = False):
@@ -327,6 +353,10 @@ class PagePool:
         self.desc = make_pages(k, v, self.refs, self.table, self.length, tokens_first)
         n = pc_pages_workspace_bytes(self.desc, table.shape[0])
         self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)
+        self._streams = set()
+
+    def _tensors(self):
+        return self.k, self.v, self.table, self.length, self.refs, self.status, self.workspace
 
     @property
     def n_heads(self) -> int:
@@ -335,7 +365,7 @@ class PagePool:
     def fork(self, parent, child, stream=None):
         """Sequences child[i], empty, take over parent[i]'s pages and length."""
         _need(parent.numel() == child.numel(), "as many parents as children")
-        with _on(self.device, stream):
+        with _on(self.device, stream, self, parent, child):
             pc_pages_fork(self.desc, _list(parent, self.device, "parent"), _list(child, self.device, "child"),
                           self.status, stream)
 
@@ -343,13 +373,13 @@ class PagePool:
         """Sequences seq[i] grow by add[i] tokens: new pages, and a copy of a
         last page that others hold too."""
         _need(seq.numel() == add.numel(), "a length for each sequence")
-        with _on(self.device, stream):
+        with _on(self.device, stream, self, seq, add):
             pc_pages_extend(self.desc, _list(seq, self.device, "seq"), _list(add, self.device, "add"), self.workspace,
                             self.status, stream)
 
     def free(self, seq, stream=None):
         """Sequences seq[i] give up their pages and are empty."""
-        with _on(self.device, stream):
+        with _on(self.device, stream, self, seq):
             pc_pages_free(self.desc, _list(seq, self.device, "seq"), self.status, stream)
 
     def compact(self, refs_to=None, table_to=None, stream=None):
@@ -361,7 +391,7 @@ class PagePool:
         _need(refs_to.numel() == self.refs.numel(), "refs_to: one for each page")
         _need(table_to.shape == self.table.shape and table_to.is_contiguous() and table_to.dtype == torch.int32
               and table_to.device == self.device, "table_to: like the table")
-        with _on(self.device, stream):
+        with _on(self.device, stream, self, refs_to, table_to):
             n_live = torch.empty(1, dtype=torch.int32, device=self.device)
             pc_pages_compact(self.desc, refs_to, table_to, n_live, self.workspace, self.status, stream)
         return n_live
@@ -373,7 +403,7 @@ class PagePool:
             self._rows(x, self.desc.n_kv_heads, "k_new and v_new")
         _need(k_new.shape == v_new.shape, "k_new and v_new are alike")
         _need(new_off.numel() == seq.numel() + 1, "new_off: one more than sequences")
-        with _on(self.device, stream):
+        with _on(self.device, stream, self, seq, new_off, k_new, v_new):
             pc_pages_write(self.desc, layer, _list(seq, self.device, "seq"), _list(new_off, self.device, "new_off"),
                            k_new.shape[0], make_rows(k_new), make_rows(v_new), self.status, stream)
 
@@ -404,13 +434,13 @@ def prefix_groups(keys, key_off, min_blocks: int = 1, stream=None) -> PrefixGrou
     _list(keys, dev, "keys", torch.int64)
     R = key_off.numel() - 1
     _need(R >= 1, "key_off: n_req + 1 offsets")
-    with _on(dev, stream):
+    with _on(dev, stream, None, keys, key_off):
         g = PrefixGroups(*torch.empty(3 * R + 3, dtype=torch.int32, device=dev).split((R, R + 1, R, 1, 1)))
         pc_prefix_groups(keys, key_off, min_blocks, *g, stream)
     return g
 
 
-class PrefixBatch:
+class PrefixBatch(_Owner):
     """Attention of a batch over a PagePool: n_req requests with n_tokens
     queries in all, of n_heads heads.  plan() once for the lengths that the
     sequences then have, attend() for every layer."""
@@ -420,6 +450,14 @@ class PrefixBatch:
         n = pc_attn_workspace_bytes(pool.desc, n_req, n_tokens, n_heads)
         self.workspace = torch.empty(n, dtype=torch.uint8, device=pool.device)
         self.workspace[:PC_ATTN_HEAD_BYTES].zero_()     # memory of a batch that is gone may hold its plan
+        self._streams = set()
+
+    def _tensors(self):
+        return self.workspace,
+
+    def _used_on(self, stream):
+        super()._used_on(stream)
+        self.pool._used_on(stream)
 
     def plan(self, seq, q_off, order=None, group_off=None, shared=None, n_groups=None, causal: bool = True,
              stream=None):
@@ -434,7 +472,7 @@ class PrefixBatch:
             _need([x.numel() for x in given] == [R, R + 1, R, 1], "groups of as many requests")
             for x in given:
                 _list(x, pool.device, "groups")
-        with _on(pool.device, stream):
+        with _on(pool.device, stream, self, seq, q_off, *given):
             pc_attn_plan(pool.desc, _list(seq, pool.device, "seq"), _list(q_off, pool.device, "q_off"), self.n_tokens,
                          self.n_heads, causal, order, group_off, shared, n_groups, self.workspace, pool.status, stream)
 
@@ -443,7 +481,7 @@ class PrefixBatch:
         over the tokens it sees; scale: 1 / sqrt(dim) unless given.  lse
         (float32 [n_tokens, n_heads]): log of each row's sum of exponentials."""
         pool = self.pool
-        with _on(pool.device, stream):
+        with _on(pool.device, stream, self, q, out, lse):
             if out is None:
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
             for x in (q, out):
