@@ -443,17 +443,23 @@ def prefix_groups(keys, key_off, min_blocks: int = 1, stream=None) -> PrefixGrou
 class PrefixBatch(_Owner):
     """Attention of a batch over a PagePool: n_req requests with n_tokens
     queries in all, of n_heads heads.  plan() once for the lengths that the
-    sequences then have, attend() for every layer."""
+    sequences then have, attend() for every layer.  What plan() finds wrong goes
+    to `status` (int32 [1], zeroed), the pool's unless given: a batch that is
+    planned on another stream than the pool's calls has one of its own, or its
+    errors stop them, and theirs it."""
 
-    def __init__(self, pool: PagePool, n_req: int, n_tokens: int, n_heads: int):
+    def __init__(self, pool: PagePool, n_req: int, n_tokens: int, n_heads: int, status=None):
         self.pool, self.n_req, self.n_tokens, self.n_heads = pool, n_req, n_tokens, n_heads
+        if status is not None:
+            _need(_list(status, pool.device, "status").numel() == 1, "status: one word")
+        self.status = status
         n = pc_attn_workspace_bytes(pool.desc, n_req, n_tokens, n_heads)
         self.workspace = torch.empty(n, dtype=torch.uint8, device=pool.device)
         self.workspace[:PC_ATTN_HEAD_BYTES].zero_()     # memory of a batch that is gone may hold its plan
         self._streams = set()
 
     def _tensors(self):
-        return self.workspace,
+        return (self.workspace,) if self.status is None else (self.workspace, self.status)
 
     def _used_on(self, stream):
         super()._used_on(stream)
@@ -474,7 +480,8 @@ class PrefixBatch(_Owner):
                 _list(x, pool.device, "groups")
         with _on(pool.device, stream, self, seq, q_off, *given):
             pc_attn_plan(pool.desc, _list(seq, pool.device, "seq"), _list(q_off, pool.device, "q_off"), self.n_tokens,
-                         self.n_heads, causal, order, group_off, shared, n_groups, self.workspace, pool.status, stream)
+                         self.n_heads, causal, order, group_off, shared, n_groups, self.workspace,
+                         pool.status if self.status is None else self.status, stream)
 
     def attend(self, layer: int, q, out=None, lse=None, scale: Optional[float] = None, stream=None):
         """softmax(scale q K^T) V for q [n_tokens, n_heads, dim], each query

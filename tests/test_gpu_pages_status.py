@@ -81,3 +81,25 @@ def test_lengths_out_of_range_stay_so(n, blocks):
     pool.status.zero_()
     pool.free(torch.arange(n, dtype=torch.int32, device=DEV))
     assert int(pool.status) == 0 and int(pool.refs.abs().sum()) == 0 and int(pool.length.abs().sum()) == 0
+
+
+def test_a_batch_with_a_status_of_its_own():
+    """What its plan refuses does not stop the pool's calls, nor theirs it."""
+    pool = pool_of(4, 3, 12)
+    seq = i32([0, 1])
+    pool.extend(seq, i32([20, 30]))
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    q = torch.ones(2, 1, 64, dtype=torch.bfloat16, device=DEV)
+    batch = dv.PrefixBatch(pool, 2, 2, 1, status=status)
+    batch.plan(i32([0, 4]), i32([0, 1, 2]))             # no such sequence
+    pool.fork(seq, i32([2, 3]))
+    assert int(status) == P.PC_EINVAL and int(pool.status) == 0 and pool.length.tolist() == [20, 30, 20, 30]
+    status.zero_()
+    pool.free(i32([0, 0]))
+    batch.plan(seq, i32([0, 1, 2]))
+    out = batch.attend(0, q)
+    assert int(status) == 0 and int(pool.status) == P.PC_EINVAL and (out == 0).all()     # V of the pool is 0
+    for bad in (torch.zeros(2, dtype=torch.int32, device=DEV), torch.zeros(1, device=DEV),
+                torch.zeros(1, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            dv.PrefixBatch(pool, 2, 2, 1, status=bad)
