@@ -296,8 +296,10 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
     block_scan<NT>(work, all_work, lds64);
     const int64_t by_wide = (all_work[0] * Hk + kWideItems - 1) / kWideItems,
                   by_narrow = (all_work[1] * Hk + kNarrowItems - 1) / kNarrowItems;
-    const int len_wide = (int)(by_wide < kWideMinBlocks ? kWideMinBlocks : by_wide);
-    const int len_narrow = (int)(by_narrow < kNarrowMinBlocks ? kNarrowMinBlocks : by_narrow);
+    // no more than the longest sequence has, for the 64-bit sums of many of these
+    constexpr int64_t kMostBlocks = (1LL << 24) * kBlk / kTileKv;
+    const int len_wide = (int)min(max(by_wide, (int64_t)kWideMinBlocks), kMostBlocks);
+    const int len_narrow = (int)min(max(by_narrow, (int64_t)kNarrowMinBlocks), kMostBlocks);
     int n_wide = 0, n_narrow = 0, rows_at = 0;
     for (int i0 = 0; i0 < n_seg; i0 += NT) {
         const int i = i0 + tid;
