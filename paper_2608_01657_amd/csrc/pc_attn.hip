@@ -845,8 +845,9 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a) {
     constexpr int kParts = 64 / kHeads, kFly = 16 / kHeads, kPer = D / 64, kTail = kFly < 8 ? 2 : 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per_query = (a.n_heads + kHeads - 1) / kHeads;
-    if (blockIdx.x == 0 && threadIdx.x < kXcds && planned(a)) a.ws.next[threadIdx.x * kNextStep] = 0;
-    const int64_t at = (int64_t)blockIdx.x * 4 + wave;
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (block == 0 && threadIdx.x < kXcds && planned(a)) a.ws.next[threadIdx.x * kNextStep] = 0;
+    const int64_t at = block * 4 + wave;
     const int64_t t = at / per_query;
     const int h0 = (int)(at - t * per_query) * kHeads;
     if (t >= a.n_tokens) return;
@@ -931,8 +932,12 @@ hipError_t launch(const AttnArgs &a, hipStream_t st) {
     // The whole attention by one / by four: 128 rows of four requests of 60,000 tokens 80 / 89 us, 2,700 rows 29 /
     // 31, 4,096 62.6 / 62.5, 9,400 34 / 32, 32,000 169 / 169.
     const int64_t rows = a.n_tokens * a.n_heads, waves = a.n_tokens * ((a.n_heads + 3) / 4);
-    if (rows <= 4096) attn_join<T, D, 1><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a);
-    else attn_join<T, D, 4><<<(uint32_t)((waves + 3) / 4), 256, 0, st>>>(a);
+    if (rows <= 4096) {
+        attn_join<T, D, 1><<<(uint32_t)((rows + 3) / 4), 256, 0, st>>>(a);
+    } else {    // a grid's row has less than 2^32 threads
+        const int64_t blocks = (waves + 3) / 4, x = blocks < 1 << 20 ? blocks : 1 << 20;
+        attn_join<T, D, 4><<<dim3((uint32_t)x, (uint32_t)((blocks + x - 1) / x)), 256, 0, st>>>(a);
+    }
     return hipGetLastError();
 }
 

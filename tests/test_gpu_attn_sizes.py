@@ -33,3 +33,25 @@ def test_a_plan_of_more_work_than_32_bits_count(new, at):
     assert n[at] == R * heads and n[1 - at] == 0
     del batch
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dim", [64])
+def test_more_rows_than_a_grid_has_threads(dim):
+    """2^26 + 5,000 queries of an empty sequence and of one that is not: zeros, a wave to a row, 2^32 threads."""
+    T, new = (1 << 26) + 5000, 3000
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        torch.cuda.empty_cache()
+    k = torch.ones(1, 4, 1, 16, dim, dtype=torch.bfloat16, device=DEV)
+    pool = dv.PagePool(k, k.clone(), n_seqs=2, table_width=2)
+    pool.extend(i32([1]), i32([20]))
+    q = torch.zeros(T, 1, dim, dtype=torch.bfloat16, device=DEV)
+    out = torch.full_like(q, 3.0)
+    batch = dv.PrefixBatch(pool, 2, T, 1)
+    batch.plan(i32([0, 1]), i32([0, T - new, T]), causal=False)
+    lse = torch.full((T, 1), 3.0, device=DEV)
+    batch.attend(0, q, out, lse)
+    assert int(pool.status) == 0
+    assert not out[:T - new].any() and (lse[:T - new] == -torch.inf).all()
+    assert (out[T - new:] == 1).all()
+    del batch, q, out, lse
+    torch.cuda.empty_cache()
