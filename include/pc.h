@@ -437,7 +437,8 @@ int32_t pc_attn_plan(const pc_pages *pages, const int32_t *d_seq, const int32_t 
 /* out[t][h] = softmax(scale * q[t][h] . K) V over the tokens that query t sees;
  * n_heads is a multiple of the KV heads, head h reads KV head
  * h / (n_heads / n_kv_heads).  n_req, n_tokens and n_heads are the plan's, and so
- * are the pool's table and lengths; K and V are of `layer`.  scale > 0.
+ * are the pool's table and lengths; K and V are of `layer`.  scale > 0, and
+ * scale log2(e) a finite float.
  *   d_lse         optional (NULL): [n_tokens][n_heads] float, the natural
  *                 logarithm of each row's sum of exponentials
  * Without a plan of these n_req, n_tokens and n_heads for this pool's shape in

@@ -186,7 +186,9 @@ int32_t pc_attn(const pc_pages *pages, int32_t layer, const pc_rows *q, int32_t 
     if (int32_t rc = check_pool(pages)) return rc;
     if (layer < 0 || layer >= pages->n_layers) return fail(PC_EINVAL, "layer %d of %d", layer, pages->n_layers);
     if (int32_t rc = check_batch(pages, n_req, n_tokens, n_heads)) return rc;
-    if (!(scale > 0) || !std::isfinite(scale)) return fail(PC_EINVAL, "scale must be positive and finite");
+    const float scale_log2 = (float)(scale * 1.4426950408889634);
+    if (!(scale > 0) || !std::isfinite(scale_log2))
+        return fail(PC_EINVAL, "scale must be positive, and scale log2(e) finite");
     if (n_tokens == 0) return ok();
     if (int32_t rc = check_rows(q, "q")) return rc;
     if (int32_t rc = check_rows(out, "out")) return rc;
@@ -214,7 +216,7 @@ int32_t pc_attn(const pc_pages *pages, int32_t layer, const pc_rows *q, int32_t 
     a.n_pages = pages->n_pages;
     a.n_heads = n_heads;
     a.group = n_heads / pages->n_kv_heads;
-    a.scale_log2 = (float)(scale * 1.4426950408889634);
+    a.scale_log2 = scale_log2;
     a.n_req = n_req;
     a.n_seqs = pages->n_seqs;
     a.head_dim = pages->head_dim;
