@@ -129,6 +129,17 @@ struct Segment {
     int32_t first;      // its first item on the wide list, or -1 - that on the narrow one
 };
 
+constexpr int kSmallGroup = 16;      // requests of a group that one thread goes through
+
+// LDS of the plan, bytes: the arrays that attn_plan declares, and those sized by the batch.
+template <int NT>
+constexpr size_t kPlanLds = NT * (sizeof(Segment) + 4) + NT / 64 * (3 * 4 + 2 * 8) + PC_MAX_BATCH / kSmallGroup * 4 +
+                            PC_MAX_BATCH / 8 + 64;
+constexpr size_t plan_lds_bytes(size_t n_req) { return 4 * (7 * n_req + 3); }
+constexpr size_t kLdsUnasked = 64 * 1024, kLdsMost = 160 * 1024;     // without an attribute, and with it
+static_assert(kPlanLds<256> + plan_lds_bytes(256) <= kLdsUnasked, "a few requests");
+static_assert(kPlanLds<1024> + plan_lds_bytes(PC_MAX_BATCH) <= kLdsMost, "the largest batch (161,804 bytes)");
+
 // The last i of n with at[i] <= x, where at[0] <= x.
 __device__ __forceinline__ int last_at(const int32_t *at, int n, int x) {
     int lo = 0;
@@ -171,7 +182,6 @@ __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
     __shared__ int32_t first_item[NT];
     __shared__ int32_t lds[3 * (NT / 64)];
     __shared__ int64_t lds64[2 * (NT / 64)];
-    constexpr int kSmallGroup = 16;
     __shared__ int large[PC_MAX_BATCH / kSmallGroup];
     __shared__ int any_bad, stop, n_large;
     __shared__ uint32_t seen[PC_MAX_BATCH / 32];
@@ -973,20 +983,19 @@ int64_t attn_ws(int32_t n_req, int64_t n_tokens, int32_t n_heads, int32_t n_kv_h
         ws->narrow = reinterpret_cast<AttnItem *>(base + nr);
         ws->o = reinterpret_cast<float *>(base + po);
         ws->lse = reinterpret_cast<float *>(base + pl);
-        ws->rows = rows;
     }
     return o;
 }
 
 hipError_t launch_attn_plan(const AttnPlanArgs &a, hipStream_t st) {
-    const size_t bytes = 4 * (7 * (size_t)a.n_req + 3);
+    const size_t bytes = plan_lds_bytes(a.n_req);
     // A barrier and a sum over 16 wavefronts cost more than what few requests have to do: with 256 / 1,024
     // threads, one request 6.1 / 7.9 us, 64 8.2 / 10.0 us, 256 10.8 / 11.1 us, 512 14.5 / 12.2 us.
     if (a.n_req <= 256) {
         attn_plan<256><<<kPlanGroups, 256, bytes, st>>>(a);
         return hipGetLastError();
     }
-    if (bytes > 16 * 1024) {    // beside the kernel's own 42 KB
+    if (kPlanLds<1024> + bytes > kLdsUnasked) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_plan<1024>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != hipSuccess) return e;

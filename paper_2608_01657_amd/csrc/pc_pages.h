@@ -90,7 +90,6 @@ struct AttnWs {
     AttnItem *wide, *narrow;
     float *o;               // [rows][head_dim] partial results, normalised
     float *lse;             // [rows] log2 of their sums of exponentials
-    int64_t rows;
 };
 constexpr int kZeroOffset = 128;
 constexpr int kWideSlots = 512;      // workgroups of the items' kernel, two to a CU

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2608_01657_amd import device as dv
+from test_gpu_attn import Batch
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -55,3 +56,9 @@ def test_more_rows_than_a_grid_has_threads(dim):
     assert (out[T - new:] == 1).all()
     del batch, q, out, lse
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("R", [256, 257, 657, 658])
+def test_batches_where_the_plan_changes_its_launch(R):
+    """The last and first numbers of requests with fewer threads, and with LDS that is not asked for."""
+    Batch([(i % 9 - 1, i % 9 if i % 9 else 0, 1 + i % 5, 1) for i in range(R)], 2, 1, 64, torch.float16).check()
