@@ -306,7 +306,8 @@ typedef struct {
     int32_t *d_len;                   /* [n_seqs] tokens, 0..16 * table_width          */
     int64_t page_stride;              /* elements from a page to the next, >= one
                                          page's 16 * n_kv_heads * head_dim, a multiple
-                                         of 8; the same for K and V                    */
+                                         of 8 (any value where n_pages is 1); the same
+                                         for K and V                                   */
     int64_t layer_stride;             /* elements from a layer to the next, a multiple
                                          of 8 (any value where n_layers is 1)          */
     int32_t n_layers;                 /* >= 1; the layers share table, len and refs    */
@@ -323,7 +324,7 @@ typedef struct {
  * aligned) for each token and head. */
 typedef struct {
     void *d_data;
-    int64_t token_stride, head_stride;   /* elements, multiples of 8 */
+    int64_t token_stride, head_stride;   /* elements, multiples of 8 (any value where there is one) */
 } pc_rows;
 
 /* Workspace bytes of pc_pages_extend for up to n sequences a call, and of

@@ -29,7 +29,7 @@ int32_t check_pool(const pc_pages *p, bool data = true) {
     if (p->layout != PC_HEADS_FIRST && p->layout != PC_TOKENS_FIRST)
         return fail(PC_EINVAL, "unknown layout %d", p->layout);
     const int64_t page = (int64_t)kBlk * p->n_kv_heads * p->head_dim;
-    if (p->page_stride < page || p->page_stride > 1LL << 40 || p->page_stride % 8)
+    if (p->n_pages > 1 && (p->page_stride < page || p->page_stride > 1LL << 40 || p->page_stride % 8))
         return fail(PC_EINVAL, "page_stride %lld: at least a page's %lld elements and a multiple of 8",
                     (long long)p->page_stride, (long long)page);
     if (p->n_layers > 1 && (p->layer_stride < page || p->layer_stride > 1LL << 46 || p->layer_stride % 8))
@@ -44,9 +44,9 @@ int32_t check_pool(const pc_pages *p, bool data = true) {
     return PC_OK;
 }
 
-int32_t check_rows(const pc_rows *r, const char *what) {
+int32_t check_rows(const pc_rows *r, int64_t tokens, int32_t heads, const char *what) {
     if (!r || !r->d_data || !aligned(r->d_data, 16)) return fail(PC_EINVAL, "%s is NULL or not 16-byte aligned", what);
-    if (r->token_stride % 8 || r->head_stride % 8)
+    if ((tokens > 1 && r->token_stride % 8) || (heads > 1 && r->head_stride % 8))
         return fail(PC_EINVAL, "%s: strides must be multiples of 8 elements", what);
     return PC_OK;
 }
@@ -136,8 +136,8 @@ int32_t pc_pages_write(const pc_pages *pages, int32_t layer, const int32_t *d_se
     if (int32_t rc = check_list(pages, n, d_seq, d_new_off, d_status)) return rc;
     if (n_tokens < 0 || n_tokens > 1 << 28) return fail(PC_EINVAL, "n_tokens %lld out of range", (long long)n_tokens);
     if (n == 0 || n_tokens == 0) return ok();
-    if (int32_t rc = check_rows(k_new, "k_new")) return rc;
-    if (int32_t rc = check_rows(v_new, "v_new")) return rc;
+    if (int32_t rc = check_rows(k_new, n_tokens, pages->n_kv_heads, "k_new")) return rc;
+    if (int32_t rc = check_rows(v_new, n_tokens, pages->n_kv_heads, "v_new")) return rc;
     return done(launch_write(*pages, layer, d_seq, d_new_off, n, n_tokens, *k_new, *v_new, d_status,
                              static_cast<hipStream_t>(stream)), "pc_pages_write");
 }
@@ -190,8 +190,8 @@ int32_t pc_attn(const pc_pages *pages, int32_t layer, const pc_rows *q, int32_t 
     if (!(scale > 0) || !std::isfinite(scale_log2))
         return fail(PC_EINVAL, "scale must be positive, and scale log2(e) finite");
     if (n_tokens == 0) return ok();
-    if (int32_t rc = check_rows(q, "q")) return rc;
-    if (int32_t rc = check_rows(out, "out")) return rc;
+    if (int32_t rc = check_rows(q, n_tokens, n_heads, "q")) return rc;
+    if (int32_t rc = check_rows(out, n_tokens, n_heads, "out")) return rc;
     if (!aligned(d_lse, 4)) return fail(PC_EINVAL, "d_lse is misaligned");
     const bool heads_first = pages->layout == PC_HEADS_FIRST;
     AttnArgs a{};

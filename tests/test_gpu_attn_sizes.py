@@ -62,3 +62,27 @@ def test_more_rows_than_a_grid_has_threads(dim):
 def test_batches_where_the_plan_changes_its_launch(R):
     """The last and first numbers of requests with fewer threads, and with LDS that is not asked for."""
     Batch([(i % 9 - 1, i % 9 if i % 9 else 0, 1 + i % 5, 1) for i in range(R)], 2, 1, 64, torch.float16).check()
+
+
+def test_one_of_a_kind_has_any_stride():
+    """One token, one head, one page: torch's strides of them are not multiples of 8."""
+    k = torch.randn(1, 16, 1, 64, 1, device=DEV).to(torch.float16).permute(0, 4, 2, 1, 3)    # one page, one head
+    v = torch.randn(1, 16, 1, 64, 1, device=DEV).to(torch.float16).permute(0, 4, 2, 1, 3)
+    assert k.stride(1) == 1
+    pool = dv.PagePool(k, v, n_seqs=1, table_width=1)
+    pool.extend(i32([0]), i32([9]))
+    new = torch.randn(1, 64, 1, device=DEV).to(torch.float16).permute(0, 2, 1)
+    assert new.stride(1) == 1
+    pool.write(0, i32([0]), i32([0, 1]), new, new)
+    assert torch.equal(k[0, 0, 0, 8], new[0, 0]) and torch.equal(v[0, 0, 0, 8], new[0, 0])
+    q = torch.randn(4, 64, 1, device=DEV).to(torch.float16).permute(2, 0, 1)     # one token
+    out = torch.zeros(4, 64, 1, device=DEV, dtype=torch.float16).permute(2, 0, 1)
+    assert q.stride(0) == 1
+    batch = dv.PrefixBatch(pool, 1, 1, 4)
+    for stream in (None, 0):
+        batch.plan(i32([0]), i32([0, 1]), stream=stream)
+        batch.attend(0, q, out, stream=stream)
+    assert int(pool.status) == 0
+    s = torch.softmax(q[0].double() @ k[0, 0, 0, :9].double().t() / 8, 1)
+    o, mag = s @ v[0, 0, 0, :9].double(), s @ v[0, 0, 0, :9].double().abs()
+    assert ((out[0].double() - o).abs() <= 2.0 ** -11 * (mag + o.abs()) + 2.0 ** -13 * mag).all()
