@@ -275,8 +275,9 @@ int32_t pc_get_stats(const void *d_stats, int32_t n_inst, int32_t instance,
  * that change it must be ordered.
  *
  * Device-side status (d_status, one int32 in device memory that the caller
- * zeroes; pc_prefix_groups alone writes one of its own): a call that finds its lists or the pool's state out of range sets
- * it to PC_EINVAL, or PC_ENOPAGES, and does nothing else unless said
+ * zeroes, while no call with it is under way; pc_prefix_groups alone writes one
+ * of its own): a call that finds its lists or the pool's state out of range
+ * sets it to PC_EINVAL, or PC_ENOPAGES, and does nothing else unless said
  * otherwise.  A call that finds it set does nothing, so that calls may be
  * queued one after another (or captured) and looked at once, at the end.
  * Calls that may overlap (on other streams) have a status of their own each, or

@@ -92,14 +92,16 @@ __device__ bool bad_pages(const pc_pages &p, uint32_t s, int at, int step) {
     return bad;
 }
 
-__device__ void fork_one(const pc_pages &p, int64_t from, int64_t to, int len, int at, int step) {
-    const int nb = blocks_of(len);
-    const int32_t *src = p.d_table + from * p.table_width;
+// Lists and page numbers have been checked, unless the caller zeroed the status
+// between two kernels of the call: none of them leads outside all the same.
+__device__ void fork_one(const pc_pages &p, uint32_t from, int64_t to, int len, int at, int step) {
+    const int nb = from < (uint32_t)p.n_seqs ? blocks_of(len) : 0;
+    const int32_t *src = p.d_table + (int64_t)from * p.table_width;
     int32_t *dst = p.d_table + to * p.table_width;
     for (int i = at; i < nb; i += step) {
         const int page = src[i];
         dst[i] = page;
-        atomicAdd(&p.d_refs[page], 1);
+        if (page_ok(p, page)) atomicAdd(&p.d_refs[page], 1);
     }
     if (at == 0) p.d_len[to] = len;
 }
@@ -107,7 +109,10 @@ __device__ void fork_one(const pc_pages &p, int64_t from, int64_t to, int len, i
 __device__ void free_one(const pc_pages &p, int64_t s, int len, int at, int step) {
     const int32_t *row = p.d_table + s * p.table_width;
     const int nb = blocks_of(len);
-    for (int i = at; i < nb; i += step) atomicSub(&p.d_refs[row[i]], 1);
+    for (int i = at; i < nb; i += step) {
+        const int page = row[i];
+        if (page_ok(p, page)) atomicSub(&p.d_refs[page], 1);
+    }
 }
 
 // Beside the length of a sequence that is about to be filled or emptied, between
