@@ -402,8 +402,9 @@ int32_t pc_prefix_groups(const uint64_t *d_keys, int64_t n_keys, const int64_t *
  * of the lengths it then has, and the attention of one layer by that plan, as
  * often as there are layers.
  *   request r     the sequence d_seq[r] (one may come twice) and the queries
- *                 d_q_off[r] .. d_q_off[r+1]-1 of n_tokens; its length L counts
- *                 the tokens of these queries, whose K and V are in the pages.
+ *                 d_q_off[r] .. d_q_off[r+1]-1 of n_tokens (from 0 to n_tokens, each
+ *                 in one request); its length L counts the tokens of these
+ *                 queries, whose K and V are in the pages.
  *   causal        query i of n sees the tokens before L - n + i + 1; otherwise,
  *                 all L.  A query that sees none (also: of an empty sequence)
  *                 gives zeros, and -inf in lse.

@@ -116,10 +116,11 @@ constexpr int kPlanGroups = 16;
 // tiles that this saves, times the tokens, outweigh what it costs: the joint
 // tiles' partial results, and the members' own ones, which without it go straight
 // to the output, written and joined.  32 heads on 8 of K and V, together / each by
-// itself: eight requests behind 4,096 shared tokens with 900 new tokens each 462 /
-// 409 us, 100: 70 / 69, 17: 21 / 25; decoding, 64 requests behind 930 tokens 22 /
-// 35, 512 behind 48 tokens 76 / 59, behind 128 80 / 72, in groups of eight behind
-// 240 90 / 82, behind 480 105 / 117, pairs behind 1,300 81 / 83.
+// itself: eight requests behind 3,300 shared tokens with 900 new tokens each 433 /
+// 409 us, 100: 63 / 67, behind 2,100 with 17: 21 / 24; decoding, 64 requests behind 930
+// tokens 21 / 30, 512 behind 48 tokens 64 / 58, behind 128 68 / 71, in groups of eight
+// behind up to 240 77 / 81, behind up to 480 88 / 116 (99 by this rule), pairs behind
+// up to 1,900 88 / 108 (99 by this rule).
 constexpr int64_t kShareCost = 16 * kTileKv, kSplitCost = 4 * kTileKv;
 
 // A segment as the plan holds it: segment i < n_req is the own tokens of the
@@ -162,7 +163,7 @@ __device__ __forceinline__ uint32_t divide(uint32_t x, uint32_t d) {
 // workgroup works all segments out by itself and writes its share of the
 // queries and items; the first one writes the rest.  128 requests with 3,000
 // items took 20 us by one workgroup, most of it to write items; by 16 they take
-// 9.
+// 11, one of them to see whether a tile's weights go in two pieces.
 template <int NT>
 __global__ __launch_bounds__(NT) void attn_plan(AttnPlanArgs a) {
     const pc_pages &p = a.p;
@@ -801,9 +802,9 @@ __device__ __forceinline__ void narrow_item(const AttnArgs &a, const AttnItem it
 // each XCD, which has an L2 of its own and takes every eighth item (workgroups go
 // round the XCDs).  Heads are the fastest index of the list, so that an XCD's
 // workgroups read the same heads' K and V, and it runs from long items to short
-// ones.  One prompt of 8,192 tokens takes 552 us in place of 800 with turns fixed
-// beforehand, one of 20,000 for 6 heads on one of K and V 587 us in place of 757,
-// 32 of 300 behind 3,000 cached ones 245 in place of 275.  Where there are no more
+// ones.  One prompt of 8,192 tokens takes 528 us in place of 800 with turns fixed
+// beforehand, one of 20,000 for 6 heads on one of K and V 570 us in place of 757,
+// 32 of 300 behind 3,000 cached ones 240 in place of 275.  Where there are no more
 // items than workgroups (with narrow ones beside them: than half of these), nothing is
 // taken.  The join leaves the counters at 0.
 template <typename T, int D>

@@ -385,7 +385,7 @@ class PagePool(_Owner):
     def compact(self, refs_to=None, table_to=None, stream=None):
         """Pages in use move to the lowest numbers; counts and tables are
         rewritten in place, or to refs_to and table_to.  Returns the number of
-        pages in use (a tensor)."""
+        pages in use (a tensor; of no meaning where the status was set)."""
         refs_to = self.refs if refs_to is None else _list(refs_to, self.device, "refs_to")
         table_to = self.table if table_to is None else table_to
         _need(refs_to.numel() == self.refs.numel(), "refs_to: one for each page")
@@ -486,7 +486,8 @@ class PrefixBatch(_Owner):
     def attend(self, layer: int, q, out=None, lse=None, scale: Optional[float] = None, stream=None):
         """softmax(scale q K^T) V for q [n_tokens, n_heads, dim], each query
         over the tokens it sees; scale: 1 / sqrt(dim) unless given.  lse
-        (float32 [n_tokens, n_heads]): log of each row's sum of exponentials."""
+        (float32 [n_tokens, n_heads]): log of each row's sum of exponentials.  Without
+        a plan, or one that was refused, out and lse stay as they are."""
         pool = self.pool
         with _on(pool.device, stream, self, q, out, lse):
             if out is None:
