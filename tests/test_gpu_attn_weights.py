@@ -75,10 +75,13 @@ def test_own_tokens(dtype, dim):
 
 
 @pytest.mark.parametrize("dtype,dim", TYPES)
-@pytest.mark.parametrize("heads,kv_heads", [(8, 2), (6, 1), (4, 4)])
+@pytest.mark.parametrize("heads,kv_heads", [(8, 2), (6, 1), (4, 4), (16, 1)])
 def test_shared_tokens(heads, kv_heads, dtype, dim):
     """Forty requests that decode behind tokens read once for all."""
-    b = batch([(0, 24, 1 + i % 37, 1 + i % 2) for i in range(40)], heads, kv_heads, dim, dtype, seed=heads)
+    new = lambda i: 1 + i % 2 * (heads // kv_heads <= 8)
+    # 16 heads a KV head: 40 tiles apart, 5 together, from 439 tokens on
+    blocks = 24 if heads // kv_heads <= 8 else 28
+    b = batch([(0, blocks, 1 + i % 37, new(i)) for i in range(40)], heads, kv_heads, dim, dtype, seed=heads)
     check(b, range(40))
     assert counts(b)[0] >= kv_heads
 

@@ -103,3 +103,33 @@ def test_a_batch_with_a_status_of_its_own():
                 torch.zeros(1, dtype=torch.int32)):
         with pytest.raises(ValueError):
             dv.PrefixBatch(pool, 2, 2, 1, status=bad)
+
+
+@pytest.mark.parametrize("n,blocks", [(3, 5), (30, 60), (40, 100), (2, 700)])
+def test_forks_and_frees_in_a_graph(n, blocks):
+    """Both ways of a fork and a free, captured, replayed between eager ones, stopped by a status that is set."""
+    pool = pool_of(3 * n, blocks, n * blocks + 3)
+    at = lambda i: torch.arange(i * n, (i + 1) * n, dtype=torch.int32, device=DEV)
+    pool.extend(at(0), i32([16 * blocks - 5] * n))
+    table = pool.table[:n].clone()
+    graphs = []
+    for f in (lambda: pool.fork(at0, at1), lambda: pool.free(at1)):
+        at0, at1 = at(0), at(1)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            f()
+        graphs.append((graph, at0, at1))
+    for step in range(4):
+        graphs[0][0].replay()
+        assert pool.length.tolist() == [16 * blocks - 5] * (2 * n) + [0] * n
+        assert torch.equal(pool.table[n:2 * n], table) and pool.refs.tolist() == [2] * (n * blocks) + [0] * 3
+        pool.fork(at(1), at(2))
+        assert torch.equal(pool.table[2 * n:], table) and int(pool.refs.max()) == 3
+        pool.status.fill_(P.PC_ENOPAGES)
+        graphs[1][0].replay()
+        assert pool.length.tolist() == [16 * blocks - 5] * (3 * n) and int(pool.status) == P.PC_ENOPAGES
+        pool.status.zero_()
+        graphs[1][0].replay()
+        pool.free(at(2))
+        assert pool.length.tolist() == [16 * blocks - 5] * n + [0] * (2 * n) and int(pool.refs.max()) == 1
+        assert int(pool.status) == 0
